@@ -252,6 +252,85 @@ int tconv_dw_backward(const tconv_desc_t *desc, const void *x, const void *w, co
                       size_t workspace_bytes, void *stream);
 
 /*
+ * Operators around the one-dimensional layers of residual networks over long signals, and activations kept in
+ * 8 bits.  Offsets are 64 bits wide.  Inputs may hold infinities and NaN: they reach the outputs that depend on them.
+ *
+ * Activations in 8 bits.  A tensor is rows x inner values (inner: the axes behind the channels; the channels
+ * where nothing is behind them).  Along a row, blocks of 32 values (the last one may be shorter) share a power
+ * of two 2^e: the smallest e >= -126 with every magnitude of the block below 127.5 * 2^e.
+ *   codes  int8  [rows][pitch], pitch = inner rounded up to a multiple of 8: x * 2^-e rounded to the nearest
+ *                whole number, halves to even (never beyond +-127); the padding of a row is 0;
+ *   scales uint8 [rows][ceil(inner / 32)]: e + 127.
+ * A value stands for code * 2^e, exact in float and in bf16, within half of 2^e of the original.  A block with a
+ * NaN or an infinity has scale 255 and codes 0, and restores to NaN throughout.
+ */
+size_t tconv_q8_codes_bytes(int64_t rows, int64_t inner);
+size_t tconv_q8_scales_bytes(int64_t rows, int64_t inner);
+int tconv_q8_store(int64_t rows, int64_t inner, int dtype, const void *x, void *codes, void *scales, void *stream);
+int tconv_q8_restore(int64_t rows, int64_t inner, int dtype, const void *codes, const void *scales, void *x,
+                     void *stream);
+
+/*
+ * Gated linear recurrence over signals [N][C][L], per row (n, c):
+ *     h_t = f_t * h_{t-1} + (1 - f_t) * x_t,   f = 1 / (1 + exp(-gate)),   h_{-1} = h0 (NULL: 0),   y_t = h_t,
+ * with gate, state and sums in fp32.  Positions of a row lie next to each other; x and gate have strides of their
+ * own between rows and between batch entries (elements), so that they can be parts of one tensor, and need only
+ * be aligned to their type.  y and grad_y are dense, grad_x and grad_gate have dense rows and one stride between
+ * batch entries.  lengths (int32 [N], NULL: all L; held to 0..L): from a row's length on its x and gate are not
+ * used, y and both gradients are 0 and the state stays.  h_last [N][C] is the state behind the last position; it
+ * may be h0 itself where L is 1.
+ *
+ * For a backward pass the forward leaves `states` (tconv_scan_states_bytes).  With the four 8-bit buffers given it
+ * also stores x and gate there (zeros behind a row's length), and the backward pass reads those in place of x
+ * and gate: its gradients are those of the recurrence over the restored values.
+ * Backward: grad_h_last may be NULL (zero); grad_h0 may be NULL.  Deterministic, no atomics.
+ */
+typedef struct {
+    int32_t N, C;
+    int64_t L;
+    int32_t dtype;                /* tconv_dtype_t of x, gate, y and their gradients */
+    int64_t x_batch, x_row;       /* strides of x between batch entries and rows */
+    int64_t gate_batch, gate_row; /* and of gate */
+    int64_t grad_batch;           /* stride of grad_x and of grad_gate between batch entries (rows are dense) */
+} tconv_scan_desc_t;
+size_t tconv_scan_states_bytes(const tconv_scan_desc_t *desc);
+size_t tconv_scan_workspace_bytes(const tconv_scan_desc_t *desc, int backward);
+int tconv_scan_forward(const tconv_scan_desc_t *desc, const void *x, const void *gate, const float *h0,
+                       const int32_t *lengths, void *y, float *h_last, float *states, void *x_codes,
+                       void *x_scales, void *gate_codes, void *gate_scales, void *workspace,
+                       size_t workspace_bytes, void *stream);
+int tconv_scan_backward(const tconv_scan_desc_t *desc, const void *x, const void *gate, const void *x_codes,
+                        const void *x_scales, const void *gate_codes, const void *gate_scales,
+                        const int32_t *lengths, const float *states, const void *grad_y,
+                        const float *grad_h_last, void *grad_x, void *grad_gate, float *grad_h0, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * Root-mean-square norm over the channels of [N][C][P] (P = 1: rows of C values), with the residual's addition:
+ *     s = x + residual, rounded to the tensors' type (residual NULL: s = x, and `sum` is not written);
+ *     rstd = 1 / sqrt(mean_c(s^2) + eps);   y = s * rstd * weight[c].
+ * y may be NULL where its 8-bit form (y_codes, y_scales) is wanted alone.  rstd (fp32 [N][P], NULL: not wanted)
+ * and s are what a backward pass needs; s_codes and s_scales, if given, take the 8-bit form of s to be kept in its
+ * place.  Backward, with z = s * rstd:
+ *     grad_x = rstd * (weight * grad_y - z * mean_c(weight * grad_y * z)) + grad_sum  (grad_sum NULL: 0),
+ * which is the gradient of the residual too, and grad_weight[c] = sum of grad_y * z (NULL: not wanted);
+ * s is NULL where s_codes and s_scales are given.  Dense tensors; fixed order of every sum, no atomics.
+ */
+typedef struct {
+    int32_t N, C;
+    int64_t P;
+    int32_t dtype; /* tconv_dtype_t of x, residual, sum, y and their gradients; weight is float [C] */
+    float eps;
+} tconv_norm_desc_t;
+size_t tconv_norm_workspace_bytes(const tconv_norm_desc_t *desc); /* of the backward pass */
+int tconv_norm_forward(const tconv_norm_desc_t *desc, const void *x, const void *residual, const float *weight,
+                       void *sum, void *y, float *rstd, void *y_codes, void *y_scales, void *s_codes,
+                       void *s_scales, void *stream);
+int tconv_norm_backward(const tconv_norm_desc_t *desc, const void *s, const void *s_codes, const void *s_scales,
+                        const float *rstd, const float *weight, const void *grad_y, const void *grad_sum,
+                        void *grad_x, float *grad_weight, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Number of operations the paper's complexity analysis (Section 4.1) assigns to
  * one forward pass of the layer: additions + comparisons + multiplications
  * (theta = 1).  Host call; 0 for an invalid descriptor.

@@ -2,7 +2,7 @@
 
 The tiled forward kernels are compiled as one translation unit per (mode, channel
 combine) family, in parallel, and linked with the API unit into one shared library.
-The autograd layer over it (csrc/torch_layers.cpp) becomes the extension module _tconv_torch.
+The autograd layer over it (csrc/torch_layers.cpp, csrc/torch_seq.cpp) becomes the extension module _tconv_torch.
 """
 from __future__ import annotations
 
@@ -31,7 +31,7 @@ FWD_INSTANCES = [("fwd_inst_maxplus_sum", 0, 1), ("fwd_inst_maxplus_max", 0, 2),
 
 def _newest_source() -> float:
     files = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cpp")) + list(CSRC.glob("*.cuh")) + \
-        list((ROOT / "include").glob("*.h")) + [Path(__file__)]
+        list(CSRC.glob("*.h")) + list((ROOT / "include").glob("*.h")) + [Path(__file__)]
     return max(f.stat().st_mtime for f in files)
 
 
@@ -78,12 +78,13 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     OBJ.mkdir(exist_ok=True)
     jobs = [(CSRC / "tconv_api.cu", OBJ / "tconv_api.o", [], verbose),
             (CSRC / "tconv_bwd_sum.cu", OBJ / "tconv_bwd_sum.o", [], verbose),
-            (CSRC / "tconv3d_api.cu", OBJ / "tconv3d_api.o", [], verbose)]
+            (CSRC / "tconv3d_api.cu", OBJ / "tconv3d_api.o", [], verbose),
+            (CSRC / "tconv_seq_api.cu", OBJ / "tconv_seq_api.o", [], verbose)]
     for name, mode, chan in FWD_INSTANCES:
         defs = [f"-DTCONV_INST_NAME={name}", f"-DTCONV_INST_MODE={mode}", f"-DTCONV_INST_CHAN={chan}"]
         jobs.append((CSRC / "tconv_fwd_inst.cu", OBJ / f"{name}.o", defs, verbose))
-    ext_obj = OBJ / "torch_layers.o"
-    jobs.append((CSRC / "torch_layers.cpp", ext_obj, [], verbose))
+    ext_objs = [OBJ / "torch_layers.o", OBJ / "torch_seq.o"]
+    jobs += [(CSRC / f"{o.stem}.cpp", o, [], verbose) for o in ext_objs]
     log = []
     with cf.ThreadPoolExecutor(max_workers=min(len(jobs), os.cpu_count() or 4)) as ex:
         for obj, rc, out in ex.map(_compile, jobs):
@@ -95,11 +96,11 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     tmp = LIB.with_suffix(f".{os.getpid()}.tmp.so")
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "--cudart", "shared"] + \
-          [str(j[1]) for j in jobs if j[1] != ext_obj] + ["-o", str(tmp)]
+          [str(j[1]) for j in jobs if j[1] not in ext_objs] + ["-o", str(tmp)]
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
     tmp = EXT.with_suffix(f".{os.getpid()}.tmp.so")
-    subprocess.run([HOST_CXX, "-shared", str(ext_obj)] + _torch_flags()[1] + ["-o", str(tmp)], check=True)
+    subprocess.run([HOST_CXX, "-shared"] + list(map(str, ext_objs)) + _torch_flags()[1] + ["-o", str(tmp)], check=True)
     os.replace(tmp, EXT)
     return LIB
 

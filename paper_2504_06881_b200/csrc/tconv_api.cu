@@ -10,6 +10,7 @@
 #include "tconv_bwd_sum.cuh"
 #include "tconv_depthwise.cuh"
 #include "tconv_generic.cuh"
+#include "tconv_internal.h"
 #include "tconv_tiled.cuh"
 
 using namespace tconv;
@@ -514,6 +515,17 @@ int dw_backward_t(const Geo& g, const void* x, const void* w, const void* w2, co
 }
 
 }  // namespace
+
+namespace tconv {
+void call_begins() { g_last_error[0] = 0; }
+int launched(int n, const char* name) {
+    const int rc = check_launch();
+    if (rc != TCONV_OK) return rc;
+    g_launches += n;
+    snprintf(g_last_kernel, sizeof(g_last_kernel), "%s", name);
+    return TCONV_OK;
+}
+}  // namespace tconv
 
 extern "C" {
 

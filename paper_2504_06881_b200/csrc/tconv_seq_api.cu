@@ -1,0 +1,200 @@
+// C ABI of the operators around the one-dimensional layers: 8-bit activations, gated linear recurrence, RMS norm.
+#include "tconv.h"
+#include "tconv_internal.h"
+#include "tconv_norm.cuh"
+#include "tconv_scan.cuh"
+
+namespace tconv {
+namespace {
+
+constexpr int64_t kMost = (int64_t)1 << 40;     // elements of a tensor
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+template <typename... P> bool all_aligned(P... p) { return (aligned16(p) && ...); }
+
+unsigned blocks_of(int64_t n, int64_t most) { return (unsigned)(n < most ? n : most); }
+
+int check_q8(int64_t rows, int64_t inner, int dtype) {
+    if (rows <= 0 || inner <= 0 || (dtype != TCONV_F32 && dtype != TCONV_BF16)) return TCONV_ERR_INVALID_ARG;
+    return rows > kMost / inner ? TCONV_ERR_TOO_LARGE : TCONV_OK;
+}
+
+template <typename T> int q8_store_t(int64_t rows, int64_t inner, const void* x, void* codes, void* scales, cudaStream_t st) {
+    const int64_t nb = rows * q8_blocks(inner);
+    q8_store_kernel<T><<<blocks_of((nb + 7) / 8, 148 * 64), 256, 0, st>>>(rows, inner, (const T*)x, (int8_t*)codes, (uint8_t*)scales);
+    return launched(1, "q8_store");
+}
+template <typename T> int q8_restore_t(int64_t rows, int64_t inner, const void* codes, const void* scales, void* x, cudaStream_t st) {
+    q8_restore_kernel<T><<<blocks_of((rows * inner + 255) / 256, 148 * 64), 256, 0, st>>>(rows, inner, (const int8_t*)codes,
+                                                                                         (const uint8_t*)scales, (T*)x);
+    return launched(1, "q8_restore");
+}
+
+int check_scan(const tconv_scan_desc_t* d, ScanArgs* a) {
+    if (!d || d->N <= 0 || d->C <= 0 || d->L <= 0 || (d->dtype != TCONV_F32 && d->dtype != TCONV_BF16))
+        return TCONV_ERR_INVALID_ARG;
+    if (d->x_batch < 0 || d->x_row < 0 || d->gate_batch < 0 || d->gate_row < 0 || d->grad_batch < 0) return TCONV_ERR_INVALID_ARG;
+    const int64_t rows = (int64_t)d->N * d->C;
+    if (rows > kMost / d->L || rows > (int64_t)INT32_MAX || d->L > (int64_t)INT32_MAX) return TCONV_ERR_TOO_LARGE;
+    *a = ScanArgs{rows, d->L, d->C, d->x_batch, d->x_row, d->gate_batch, d->gate_row, d->grad_batch, nullptr};
+    return TCONV_OK;
+}
+
+int64_t scan_chunks(const ScanArgs& a) { return (a.L + kScanChunk - 1) / kScanChunk; }
+
+template <typename T>
+int scan_fwd_t(const ScanArgs& a, const void* x, const void* gate, const float* h0, void* y, float* h_last, float* states,
+               void* xc, void* xs, void* gc, void* gs, cudaStream_t st) {
+    const unsigned grid = (unsigned)((a.rows + 63) / 64);
+    const auto kern = xc ? scan_fwd_row_kernel<T, true> : scan_fwd_row_kernel<T, false>;
+    kern<<<grid, 64, 0, st>>>(a, (const T*)x, (const T*)gate, h0, (T*)y, h_last, states, (int8_t*)xc, (uint8_t*)xs, (int8_t*)gc,
+                              (uint8_t*)gs);
+    return launched(1, "scan_fwd");
+}
+template <typename T>
+int scan_bwd_t(const ScanArgs& a, const void* x, const void* gate, const void* xc, const void* xs, const void* gc, const void* gs,
+               const float* states, const void* gy, const float* gh, void* gx, void* gg, float* gh0, cudaStream_t st) {
+    const unsigned grid = (unsigned)((a.rows + 63) / 64);
+    const auto kern = xc ? scan_bwd_row_kernel<T, true> : scan_bwd_row_kernel<T, false>;
+    kern<<<grid, 64, 0, st>>>(a, (const T*)x, (const T*)gate, (const int8_t*)xc, (const uint8_t*)xs, (const int8_t*)gc,
+                              (const uint8_t*)gs, states, (const T*)gy, gh, (T*)gx, (T*)gg, gh0);
+    return launched(1, "scan_bwd");
+}
+
+int check_norm(const tconv_norm_desc_t* d, NormArgs* a) {
+    if (!d || d->N <= 0 || d->C <= 0 || d->P <= 0 || (d->dtype != TCONV_F32 && d->dtype != TCONV_BF16) || !(d->eps >= 0))
+        return TCONV_ERR_INVALID_ARG;
+    if ((int64_t)d->N * d->C > kMost / d->P || (int64_t)d->N > (int64_t)INT32_MAX * 32 / d->P) return TCONV_ERR_TOO_LARGE;
+    *a = NormArgs{d->N, d->C, d->P, d->eps};
+    return TCONV_OK;
+}
+
+template <typename T>
+int norm_fwd_t(const NormArgs& a, const void* x, const void* r, const float* w, const NormOut& o, cudaStream_t st) {
+    if (a.P > 1)
+        norm_fwd_cols_kernel<T><<<(unsigned)((q8_blocks(a.P) * a.N + 3) / 4), 128, 0, st>>>(a, (const T*)x, (const T*)r, w, o);
+    else
+        norm_fwd_rows_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, (const T*)x, (const T*)r, w, o);
+    return launched(1, "norm_fwd");
+}
+template <typename T> int norm_bwd_t(const NormArgs& a, const NormIn& k, void* gx, float* gw, cudaStream_t st) {
+    if (a.P > 1)
+        norm_bwd_cols_kernel<T><<<(unsigned)((a.P * a.N + 127) / 128), 128, 0, st>>>(a, k, (T*)gx);
+    else
+        norm_bwd_rows_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, k, (T*)gx);
+    const int rc = launched(1, "norm_bwd");
+    if (rc || !gw) return rc;
+    norm_bwd_weight_kernel<T><<<(unsigned)a.C, 256, 0, st>>>(a, k, gw);
+    return launched(1, "norm_bwd");
+}
+
+}  // namespace
+}  // namespace tconv
+
+using namespace tconv;
+
+extern "C" {
+
+size_t tconv_q8_codes_bytes(int64_t rows, int64_t inner) {
+    return check_q8(rows, inner, TCONV_F32) ? 0 : (size_t)(rows * q8_pitch(inner));
+}
+size_t tconv_q8_scales_bytes(int64_t rows, int64_t inner) {
+    return check_q8(rows, inner, TCONV_F32) ? 0 : (size_t)(rows * q8_blocks(inner));
+}
+
+int tconv_q8_store(int64_t rows, int64_t inner, int dtype, const void* x, void* codes, void* scales, void* stream) {
+    const int rc = check_q8(rows, inner, dtype);
+    if (rc) return rc;
+    if (!x || !codes || !scales) return TCONV_ERR_INVALID_ARG;
+    if (!all_aligned(x, codes, scales)) return TCONV_ERR_MISALIGNED;
+    call_begins();
+    return (dtype == TCONV_F32 ? q8_store_t<float> : q8_store_t<__nv_bfloat16>)(rows, inner, x, codes, scales, (cudaStream_t)stream);
+}
+
+int tconv_q8_restore(int64_t rows, int64_t inner, int dtype, const void* codes, const void* scales, void* x, void* stream) {
+    const int rc = check_q8(rows, inner, dtype);
+    if (rc) return rc;
+    if (!x || !codes || !scales) return TCONV_ERR_INVALID_ARG;
+    if (!all_aligned(x, codes, scales)) return TCONV_ERR_MISALIGNED;
+    call_begins();
+    return (dtype == TCONV_F32 ? q8_restore_t<float> : q8_restore_t<__nv_bfloat16>)(rows, inner, codes, scales, x, (cudaStream_t)stream);
+}
+
+size_t tconv_scan_states_bytes(const tconv_scan_desc_t* desc) {
+    ScanArgs a;
+    return check_scan(desc, &a) ? 0 : (size_t)(a.rows * scan_chunks(a)) * sizeof(float);
+}
+
+size_t tconv_scan_workspace_bytes(const tconv_scan_desc_t*, int) { return 0; }
+
+int tconv_scan_forward(const tconv_scan_desc_t* desc, const void* x, const void* gate, const float* h0, const int32_t* lengths,
+                       void* y, float* h_last, float* states, void* x_codes, void* x_scales, void* gate_codes, void* gate_scales,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+    ScanArgs a;
+    const int rc = check_scan(desc, &a);
+    if (rc) return rc;
+    const int kept = !!x_codes + !!x_scales + !!gate_codes + !!gate_scales;
+    if (!x || !gate || !y || !h_last || (kept != 0 && kept != 4) || (kept && !states)) return TCONV_ERR_INVALID_ARG;
+    if (h_last == h0 && a.L > 1) return TCONV_ERR_INVALID_ARG;
+    if (!all_aligned(y, h0, h_last, states, x_codes, x_scales, gate_codes, gate_scales, lengths, workspace)) return TCONV_ERR_MISALIGNED;
+    const uintptr_t es = desc->dtype == TCONV_F32 ? 4 : 2;
+    if ((uintptr_t)x % es || (uintptr_t)gate % es) return TCONV_ERR_MISALIGNED;
+    if (workspace_bytes < tconv_scan_workspace_bytes(desc, 0)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
+    a.lengths = lengths;
+    call_begins();
+    return (desc->dtype == TCONV_F32 ? scan_fwd_t<float> : scan_fwd_t<__nv_bfloat16>)(
+        a, x, gate, h0, y, h_last, states, x_codes, x_scales, gate_codes, gate_scales, (cudaStream_t)stream);
+}
+
+int tconv_scan_backward(const tconv_scan_desc_t* desc, const void* x, const void* gate, const void* x_codes, const void* x_scales,
+                        const void* gate_codes, const void* gate_scales, const int32_t* lengths, const float* states,
+                        const void* grad_y, const float* grad_h_last, void* grad_x, void* grad_gate, float* grad_h0,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    ScanArgs a;
+    const int rc = check_scan(desc, &a);
+    if (rc) return rc;
+    const int kept = !!x_codes + !!x_scales + !!gate_codes + !!gate_scales;
+    if ((kept != 4 && (kept != 0 || !x || !gate)) || !states || !grad_y || !grad_x || !grad_gate) return TCONV_ERR_INVALID_ARG;
+    if (desc->grad_batch < desc->C * a.L && desc->N > 1) return TCONV_ERR_INVALID_ARG;
+    if (!all_aligned(x_codes, x_scales, gate_codes, gate_scales, lengths, states, grad_y, grad_h_last, grad_h0, workspace))
+        return TCONV_ERR_MISALIGNED;
+    const uintptr_t es = desc->dtype == TCONV_F32 ? 4 : 2;
+    if ((uintptr_t)x % es || (uintptr_t)gate % es || (uintptr_t)grad_x % es || (uintptr_t)grad_gate % es) return TCONV_ERR_MISALIGNED;
+    if (workspace_bytes < tconv_scan_workspace_bytes(desc, 1)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
+    a.lengths = lengths;
+    call_begins();
+    return (desc->dtype == TCONV_F32 ? scan_bwd_t<float> : scan_bwd_t<__nv_bfloat16>)(
+        a, x, gate, x_codes, x_scales, gate_codes, gate_scales, states, grad_y, grad_h_last, grad_x, grad_gate, grad_h0,
+        (cudaStream_t)stream);
+}
+
+size_t tconv_norm_workspace_bytes(const tconv_norm_desc_t*) { return 0; }
+
+int tconv_norm_forward(const tconv_norm_desc_t* desc, const void* x, const void* residual, const float* weight, void* sum, void* y,
+                       float* rstd, void* y_codes, void* y_scales, void* s_codes, void* s_scales, void* stream) {
+    NormArgs a;
+    const int rc = check_norm(desc, &a);
+    if (rc) return rc;
+    if (!x || !weight || !y_codes != !y_scales || !s_codes != !s_scales || (!y && !y_codes) || !residual != !sum)
+        return TCONV_ERR_INVALID_ARG;
+    if (!all_aligned(x, residual, weight, sum, y, rstd, y_codes, y_scales, s_codes, s_scales)) return TCONV_ERR_MISALIGNED;
+    const NormOut o{sum, y, rstd, (int8_t*)y_codes, (uint8_t*)y_scales, (int8_t*)s_codes, (uint8_t*)s_scales};
+    call_begins();
+    return (desc->dtype == TCONV_F32 ? norm_fwd_t<float> : norm_fwd_t<__nv_bfloat16>)(a, x, residual, weight, o, (cudaStream_t)stream);
+}
+
+int tconv_norm_backward(const tconv_norm_desc_t* desc, const void* s, const void* s_codes, const void* s_scales, const float* rstd,
+                        const float* weight, const void* grad_y, const void* grad_sum, void* grad_x, float* grad_weight,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    NormArgs a;
+    const int rc = check_norm(desc, &a);
+    if (rc) return rc;
+    if (!s_codes != !s_scales || !s == !s_codes || !rstd || !weight || !grad_y || !grad_x) return TCONV_ERR_INVALID_ARG;
+    if (!all_aligned(s, s_codes, s_scales, rstd, weight, grad_y, grad_sum, grad_x, grad_weight, workspace)) return TCONV_ERR_MISALIGNED;
+    if (workspace_bytes < tconv_norm_workspace_bytes(desc)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
+    const NormIn k{s, (const int8_t*)s_codes, (const uint8_t*)s_scales, rstd, weight, grad_y, grad_sum};
+    call_begins();
+    return (desc->dtype == TCONV_F32 ? norm_bwd_t<float> : norm_bwd_t<__nv_bfloat16>)(a, k, grad_x, grad_weight, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -15,18 +15,13 @@
 
 #include "tconv.h"
 #include "tconv3d.h"
+#include "torch_common.h"
 
 namespace {
-
-using at::Tensor;
-using torch::autograd::AutogradContext;
-using torch::autograd::Variable;
-using torch::autograd::variable_list;
-
 PyObject* g_error = nullptr;   // the binding's TconvError(status, where)
+}
 
-// Raises TconvError; callable without the GIL (the autograd engine's threads).
-[[noreturn]] void fail(int rc, const char* where) {
+void tconv_torch::fail(int rc, const char* where) {
     pybind11::gil_scoped_acquire gil;
     pybind11::object e = pybind11::reinterpret_borrow<pybind11::object>(g_error)(rc, where);
     PyErr_SetObject(g_error, e.ptr());
@@ -34,6 +29,14 @@ PyObject* g_error = nullptr;   // the binding's TconvError(status, where)
     err.persist();
     throw std::move(err);
 }
+
+namespace {
+
+using at::Tensor;
+using torch::autograd::AutogradContext;
+using torch::autograd::Variable;
+using torch::autograd::variable_list;
+using tconv_torch::fail;
 
 enum Kind { kDense = 0, kDepthwise = 1, kVolume = 2 };
 
@@ -289,4 +292,5 @@ PYBIND11_MODULE(_tconv_torch, m) {
     }));
     m.def("set_error", [](pybind11::object e) { g_error = e.release().ptr(); });
     m.def("layer", &layer, pybind11::call_guard<pybind11::gil_scoped_release>());
+    tconv_torch::bind_seq(m);
 }

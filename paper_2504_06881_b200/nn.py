@@ -10,11 +10,12 @@ arguments as ``nn.Conv2d``; ``mode`` selects max_plus / min_plus / compound / pa
 from __future__ import annotations
 
 import math
+from typing import NamedTuple, Optional
 
 import torch
 import torch.nn as nn
 
-from . import tconv, tconv3d
+from . import tconv, tconv3d, tseq  # noqa: F401
 try:
     from . import _tconv_torch as _native
 except ImportError as err:
@@ -534,3 +535,97 @@ class TropicalConv1d(nn.Module):
         N, C, L = x.shape
         y = self.conv(x.reshape(N, C, 1, 1, L))
         return y.reshape(N, y.shape[1], y.shape[4])
+
+
+class Q8(NamedTuple):
+    """A tensor kept in 8 bits: blocks of 32 values along a row (what lies behind the channel axis; the channels where
+    nothing does) share a power of two, the smallest 2^e, e >= -126, with every magnitude below 127.5 * 2^e; a value is
+    code * 2^e.  A block with a NaN or an infinity restores to NaN.  codes: int8 [rows, inner rounded up to 8]; scales:
+    uint8 [rows, blocks], e + 127."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    shape: tuple
+    dtype: torch.dtype
+
+    def restore(self, dtype=None):
+        """The values, in the type of the tensor that was stored or in `dtype` (float32, bfloat16; exact in both)."""
+        return _native.q8_restore(self.codes, self.scales, self.shape, _q8_type(dtype or self.dtype))
+
+    @property
+    def nbytes(self):
+        return self.codes.nbytes + self.scales.nbytes
+
+
+def _q8_type(dtype):
+    for name, t in tconv.TORCH_DTYPE.items():
+        if t == dtype:
+            return tconv.DTYPES[name]
+    raise ValueError(f"dtype: need float32 or bfloat16, got {dtype}")
+
+
+def _kept(checkpoint):
+    if checkpoint not in (None, "q8"):
+        raise ValueError(f"checkpoint must be None or 'q8', got {checkpoint!r}")
+    return checkpoint == "q8"
+
+
+def q8_store(x) -> Q8:
+    """x (float32 or bfloat16, on the GPU) in 8 bits; no gradients."""
+    codes, scales = _native.q8_store(x)
+    return Q8(codes, scales, tuple(x.shape), x.dtype)
+
+
+def gated_scan(x, gate=None, h0=None, lengths=None, checkpoint=None):
+    """Gated linear recurrence h_t = f_t h_{t-1} + (1 - f_t) x_t, f = sigmoid(gate), along the last axis of x [N, C, L].
+
+    gate: [N, C, L], x's type; without it x is [N, 2C, L] and its second half holds the gates (the two halves of one
+    convolution's output, read and differentiated in place).  h0: float32 [N, C], zero if absent.  lengths: integers
+    [N]; from a row's length on y is zero and the state stays.  checkpoint="q8": what the backward pass needs of x and
+    gate is kept in 8 bits (see Q8) and its gradients are those of the recurrence over the restored values; the
+    forward is unchanged.  Returns y [N, C, L] and the last state, float32 [N, C]."""
+    return _native.gated_scan(x, gate, h0, lengths, _kept(checkpoint))
+
+
+def gated_scan_step(h, x, gate=None, out=None):
+    """One position of gated_scan for streaming: state h float32 [N, C], x and gate [N, C] (or x [N, 2C] alone).
+    Returns y and the new state, written to `out` if given, which may be h.  Records no gradients."""
+    return _native.gated_scan_step(h, x, gate, out)
+
+
+class NormOutput(NamedTuple):
+    y: Optional[torch.Tensor]
+    stream: torch.Tensor
+    q8: Optional[Q8]
+
+
+_OUTPUTS = {"same": 0, "q8": 1, "both": 2}
+
+
+def rms_norm(x, weight, residual=None, eps=1e-6, output="same", checkpoint=None) -> NormOutput:
+    """Root-mean-square norm over the channels of x [N, C, ...] with the residual's addition: stream = x + residual
+    (rounded to x's type; x itself without a residual), y = stream / sqrt(mean_c(stream^2) + eps) * weight[c].
+
+    output: "same" (y), "q8" (y in 8 bits alone; no gradients) or "both".  checkpoint="q8": the backward pass keeps
+    the stream in 8 bits (see Q8) in place of the tensor itself."""
+    if output not in _OUTPUTS:
+        raise ValueError(f"output must be one of {tuple(_OUTPUTS)}, got {output!r}")
+    y, s, codes, scales = _native.rms_norm(x, weight, residual, eps, _OUTPUTS[output], _kept(checkpoint))
+    return NormOutput(y, x if s is None else s, None if codes is None else Q8(codes, scales, tuple(x.shape), x.dtype))
+
+
+class RMSNorm(nn.Module):
+    """rms_norm over the channels with a learned weight.  forward(x) gives y; forward(x, residual) gives y and the new
+    stream."""
+
+    def __init__(self, channels, eps=1e-6, checkpoint=None):
+        super().__init__()
+        _kept(checkpoint)
+        self.channels, self.eps, self.checkpoint = channels, eps, checkpoint
+        self.weight = nn.Parameter(torch.ones(channels))
+
+    def extra_repr(self):
+        return f"{self.channels}, eps={self.eps}, checkpoint={self.checkpoint}"
+
+    def forward(self, x, residual=None):
+        r = rms_norm(x, self.weight, residual, self.eps, checkpoint=self.checkpoint)
+        return r.y if residual is None else (r.y, r.stream)

@@ -28,7 +28,10 @@ SYMBOLS = ("tconv_output_shape", "tconv_winner_bytes", "tconv_workspace_bytes", 
            "tconv_backward", "tconv_forward_stats", "tconv_stats_workspace_bytes", "tconv_forward_noalloc", "tconv_forward_noalloc_max_scratch", "tconv_paper_ops", "tconv_alu_probe", "tconv_alu_probe_name",
            "tconv_device_status", "tconv_status_string", "tconv_last_error", "tconv_last_kernel",
            "tconv_launch_count", "tconv_dw_winner_bytes", "tconv_dw_workspace_bytes", "tconv_dw_forward",
-           "tconv_dw_backward")
+           "tconv_dw_backward",
+           "tconv_q8_codes_bytes", "tconv_q8_scales_bytes", "tconv_q8_store", "tconv_q8_restore",
+           "tconv_scan_states_bytes", "tconv_scan_workspace_bytes", "tconv_scan_forward", "tconv_scan_backward",
+           "tconv_norm_workspace_bytes", "tconv_norm_forward", "tconv_norm_backward")
 
 
 class TconvError(RuntimeError):
