@@ -4,6 +4,8 @@
 #include "tconv_norm.cuh"
 #include "tconv_scan.cuh"
 
+#include <type_traits>
+
 namespace tconv {
 namespace {
 
@@ -30,35 +32,69 @@ template <typename T> int q8_restore_t(int64_t rows, int64_t inner, const void* 
     return launched(1, "q8_restore");
 }
 
-int check_scan(const tconv_scan_desc_t* d, ScanArgs* a) {
+int check_scan(const tconv_scan_desc_t* d, ScanArgs* a, ScanPlan* p) {
     if (!d || d->N <= 0 || d->C <= 0 || d->L <= 0 || (d->dtype != TCONV_F32 && d->dtype != TCONV_BF16))
         return TCONV_ERR_INVALID_ARG;
     if (d->x_batch < 0 || d->x_row < 0 || d->gate_batch < 0 || d->gate_row < 0 || d->grad_batch < 0) return TCONV_ERR_INVALID_ARG;
     const int64_t rows = (int64_t)d->N * d->C;
+    // (positions of a row are counted in 32 bits, a few chunks beyond its end among them)
     if (rows > kMost / d->L || rows > (int64_t)INT32_MAX || d->L > (int64_t)INT32_MAX) return TCONV_ERR_TOO_LARGE;
-    *a = ScanArgs{rows, d->L, d->C, d->x_batch, d->x_row, d->gate_batch, d->gate_row, d->grad_batch, nullptr};
+    *p = plan_scan(rows, d->L);
+    *a = ScanArgs{rows, (uint32_t)d->L, (uint32_t)((d->L + kScanChunk - 1) / kScanChunk), p->per_part, d->C, p->parts,
+                  d->x_batch, d->x_row, d->gate_batch, d->gate_row, d->grad_batch, nullptr, nullptr};
     return TCONV_OK;
 }
 
-int64_t scan_chunks(const ScanArgs& a) { return (a.L + kScanChunk - 1) / kScanChunk; }
+size_t scan_workspace(const ScanArgs& a) { return a.parts > 1 ? (size_t)(a.rows * a.parts) * sizeof(float4) : 0; }
 
-template <typename T>
-int scan_fwd_t(const ScanArgs& a, const void* x, const void* gate, const float* h0, void* y, float* h_last, float* states,
-               void* xc, void* xs, void* gc, void* gs, cudaStream_t st) {
-    const unsigned grid = (unsigned)((a.rows + 63) / 64);
-    const auto kern = xc ? scan_fwd_row_kernel<T, true> : scan_fwd_row_kernel<T, false>;
-    kern<<<grid, 64, 0, st>>>(a, (const T*)x, (const T*)gate, h0, (T*)y, h_last, states, (int8_t*)xc, (uint8_t*)xs, (int8_t*)gc,
-                              (uint8_t*)gs);
-    return launched(1, "scan_fwd");
+// Rows that all start on 16 bytes, and whose length is whole vectors (so that no vector reaches into the next row).
+bool rows_aligned(const void* p, int64_t batch, int64_t row, int64_t L, int64_t per) {
+    return aligned16(p) && batch % per == 0 && row % per == 0 && L % per == 0;
 }
-template <typename T>
-int scan_bwd_t(const ScanArgs& a, const void* x, const void* gate, const void* xc, const void* xs, const void* gc, const void* gs,
-               const float* states, const void* gy, const float* gh, void* gx, void* gg, float* gh0, cudaStream_t st) {
-    const unsigned grid = (unsigned)((a.rows + 63) / 64);
-    const auto kern = xc ? scan_bwd_row_kernel<T, true> : scan_bwd_row_kernel<T, false>;
-    kern<<<grid, 64, 0, st>>>(a, (const T*)x, (const T*)gate, (const int8_t*)xc, (const uint8_t*)xs, (const int8_t*)gc,
-                              (const uint8_t*)gs, states, (const T*)gy, gh, (T*)gx, (T*)gg, gh0);
-    return launched(1, "scan_bwd");
+
+enum { kFwd, kBwd };
+
+template <int DIR, typename T, bool Q8, int ACC, int G, bool MULTI, bool JOIN, typename IO>
+void scan_launch(const ScanArgs& a, const ScanPlan& p, const IO& io, cudaStream_t st) {
+    const auto kern = [] {
+        if constexpr (DIR == kFwd) return scan_fwd_kernel<T, Q8, ACC, G, MULTI, JOIN>;
+        else return scan_bwd_kernel<T, Q8, ACC, G, MULTI, JOIN>;
+    }();
+    if constexpr (MULTI) {
+        kern<<<dim3((unsigned)a.rows, (unsigned)p.parts), p.warps * 32, 0, st>>>(a, io);
+    } else {
+        const int64_t per = 4 * (32 / G);
+        kern<<<(unsigned)((a.rows + per - 1) / per), 128, 0, st>>>(a, io);
+    }
+}
+
+template <int DIR, typename T, bool Q8, bool VEC, typename IO>
+int scan_run(const ScanArgs& a, const ScanPlan& p, const IO& io, cudaStream_t st) {
+    constexpr int kLong = VEC ? kVector : kStaged, kShort = VEC ? kVector : kStraight;
+    const char* name = DIR == kFwd ? "scan_fwd" : "scan_bwd";
+    if (p.g == 1) scan_launch<DIR, T, Q8, kShort, 1, false, false>(a, p, io, st);
+    else if (p.g == 4) scan_launch<DIR, T, Q8, kShort, 4, false, false>(a, p, io, st);
+    else if (p.g == 16) scan_launch<DIR, T, Q8, kShort, 16, false, false>(a, p, io, st);
+    else if (p.warps == 1) scan_launch<DIR, T, Q8, kLong, 32, false, false>(a, p, io, st);
+    else {
+        if (p.parts > 1) {
+            scan_launch<DIR, T, Q8, kLong, 32, true, true>(a, p, io, st);
+            const int rc = launched(1, name);
+            if (rc) return rc;
+        }
+        scan_launch<DIR, T, Q8, kLong, 32, true, false>(a, p, io, st);
+    }
+    return launched(1, name);
+}
+
+template <int DIR, typename IO>
+int scan_any(const ScanArgs& a, const ScanPlan& p, const IO& io, int dtype, bool q8, bool vec, cudaStream_t st) {
+    const auto go = [&](auto type, auto kept) {
+        using T = decltype(type);
+        return vec ? scan_run<DIR, T, decltype(kept)::value, true>(a, p, io, st) : scan_run<DIR, T, decltype(kept)::value, false>(a, p, io, st);
+    };
+    if (dtype == TCONV_F32) return q8 ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});
+    return q8 ? go(__nv_bfloat16{}, std::true_type{}) : go(__nv_bfloat16{}, std::false_type{});
 }
 
 int check_norm(const tconv_norm_desc_t* d, NormArgs* a) {
@@ -122,28 +158,38 @@ int tconv_q8_restore(int64_t rows, int64_t inner, int dtype, const void* codes, 
 
 size_t tconv_scan_states_bytes(const tconv_scan_desc_t* desc) {
     ScanArgs a;
-    return check_scan(desc, &a) ? 0 : (size_t)(a.rows * scan_chunks(a)) * sizeof(float);
+    ScanPlan p;
+    return check_scan(desc, &a, &p) ? 0 : (size_t)(a.rows * a.chunks) * sizeof(float);
 }
 
-size_t tconv_scan_workspace_bytes(const tconv_scan_desc_t*, int) { return 0; }
+size_t tconv_scan_workspace_bytes(const tconv_scan_desc_t* desc, int) {
+    ScanArgs a;
+    ScanPlan p;
+    return check_scan(desc, &a, &p) ? 0 : scan_workspace(a);
+}
 
 int tconv_scan_forward(const tconv_scan_desc_t* desc, const void* x, const void* gate, const float* h0, const int32_t* lengths,
                        void* y, float* h_last, float* states, void* x_codes, void* x_scales, void* gate_codes, void* gate_scales,
                        void* workspace, size_t workspace_bytes, void* stream) {
     ScanArgs a;
-    const int rc = check_scan(desc, &a);
+    ScanPlan p;
+    const int rc = check_scan(desc, &a, &p);
     if (rc) return rc;
     const int kept = !!x_codes + !!x_scales + !!gate_codes + !!gate_scales;
     if (!x || !gate || !y || !h_last || (kept != 0 && kept != 4) || (kept && !states)) return TCONV_ERR_INVALID_ARG;
     if (h_last == h0 && a.L > 1) return TCONV_ERR_INVALID_ARG;
     if (!all_aligned(y, h0, h_last, states, x_codes, x_scales, gate_codes, gate_scales, lengths, workspace)) return TCONV_ERR_MISALIGNED;
-    const uintptr_t es = desc->dtype == TCONV_F32 ? 4 : 2;
+    const int es = desc->dtype == TCONV_F32 ? 4 : 2;
     if ((uintptr_t)x % es || (uintptr_t)gate % es) return TCONV_ERR_MISALIGNED;
-    if (workspace_bytes < tconv_scan_workspace_bytes(desc, 0)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = scan_workspace(a);
+    if (workspace_bytes < need || (need && !workspace)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
     a.lengths = lengths;
+    a.joined = (float4*)workspace;
+    const int64_t per = 16 / es;
+    const bool vec = rows_aligned(x, a.xb, a.xr, a.L, per) && rows_aligned(gate, a.gb, a.gr, a.L, per);
+    const ScanFwd io{x, gate, h0, y, h_last, states, (int8_t*)x_codes, (int8_t*)gate_codes, (uint8_t*)x_scales, (uint8_t*)gate_scales};
     call_begins();
-    return (desc->dtype == TCONV_F32 ? scan_fwd_t<float> : scan_fwd_t<__nv_bfloat16>)(
-        a, x, gate, h0, y, h_last, states, x_codes, x_scales, gate_codes, gate_scales, (cudaStream_t)stream);
+    return scan_any<kFwd>(a, p, io, desc->dtype, kept, vec, (cudaStream_t)stream);
 }
 
 int tconv_scan_backward(const tconv_scan_desc_t* desc, const void* x, const void* gate, const void* x_codes, const void* x_scales,
@@ -151,21 +197,27 @@ int tconv_scan_backward(const tconv_scan_desc_t* desc, const void* x, const void
                         const void* grad_y, const float* grad_h_last, void* grad_x, void* grad_gate, float* grad_h0,
                         void* workspace, size_t workspace_bytes, void* stream) {
     ScanArgs a;
-    const int rc = check_scan(desc, &a);
+    ScanPlan p;
+    const int rc = check_scan(desc, &a, &p);
     if (rc) return rc;
     const int kept = !!x_codes + !!x_scales + !!gate_codes + !!gate_scales;
     if ((kept != 4 && (kept != 0 || !x || !gate)) || !states || !grad_y || !grad_x || !grad_gate) return TCONV_ERR_INVALID_ARG;
-    if (desc->grad_batch < desc->C * a.L && desc->N > 1) return TCONV_ERR_INVALID_ARG;
+    if (desc->grad_batch < desc->C * desc->L && desc->N > 1) return TCONV_ERR_INVALID_ARG;
     if (!all_aligned(x_codes, x_scales, gate_codes, gate_scales, lengths, states, grad_y, grad_h_last, grad_h0, workspace))
         return TCONV_ERR_MISALIGNED;
-    const uintptr_t es = desc->dtype == TCONV_F32 ? 4 : 2;
+    const int es = desc->dtype == TCONV_F32 ? 4 : 2;
     if ((uintptr_t)x % es || (uintptr_t)gate % es || (uintptr_t)grad_x % es || (uintptr_t)grad_gate % es) return TCONV_ERR_MISALIGNED;
-    if (workspace_bytes < tconv_scan_workspace_bytes(desc, 1)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = scan_workspace(a);
+    if (workspace_bytes < need || (need && !workspace)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
     a.lengths = lengths;
+    a.joined = (float4*)workspace;
+    const int64_t per = 16 / es;
+    const bool vec = rows_aligned(grad_x, a.ob, a.L, a.L, per) && rows_aligned(grad_gate, a.ob, a.L, a.L, per) &&
+                     (kept || (rows_aligned(x, a.xb, a.xr, a.L, per) && rows_aligned(gate, a.gb, a.gr, a.L, per)));
+    const ScanBwd io{x, gate, (const int8_t*)x_codes, (const int8_t*)gate_codes, (const uint8_t*)x_scales, (const uint8_t*)gate_scales,
+                     states, grad_y, grad_h_last, grad_x, grad_gate, grad_h0};
     call_begins();
-    return (desc->dtype == TCONV_F32 ? scan_bwd_t<float> : scan_bwd_t<__nv_bfloat16>)(
-        a, x, gate, x_codes, x_scales, gate_codes, gate_scales, states, grad_y, grad_h_last, grad_x, grad_gate, grad_h0,
-        (cudaStream_t)stream);
+    return scan_any<kBwd>(a, p, io, desc->dtype, kept, vec, (cudaStream_t)stream);
 }
 
 size_t tconv_norm_workspace_bytes(const tconv_norm_desc_t*) { return 0; }
