@@ -33,29 +33,139 @@ __device__ __forceinline__ int q8_code(float v, uint32_t byte) {
     return byte == 255u ? 0 : __float2int_rn(v * q8_inverse(byte));
 }
 
-// One warp per block.
-template <typename T>
+// Scale byte of the block that v is part of: a thread has eight values of it, and its four threads are neighbours (G = 1: a row
+// of at most eight values, one thread's).
+template <int G> __device__ __forceinline__ uint32_t block_scale(const float (&v)[8]) {
+    uint32_t top = magnitude_bits(v[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = max(top, magnitude_bits(v[i]));
+    if constexpr (G > 1) {
+        top = max(top, __shfl_xor_sync(~0u, top, 1));
+        top = max(top, __shfl_xor_sync(~0u, top, 2));
+    }
+    return q8_scale_byte(top);
+}
+// v becomes the values its codes stand for.  Rounded by adding 1.5 * 2^23, whose unit is 1: the code is the sum's low byte.
+__device__ __forceinline__ uint2 encode_eight(float (&v)[8], uint32_t byte) {
+    const float inv = q8_inverse(byte), unit = q8_unit(byte), magic = 12582912.0f;
+    uint32_t b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float r = byte == 255u ? magic : __fadd_rn(__fmul_rn(v[i], inv), magic);
+        b[i] = __float_as_uint(r);
+        v[i] = __fsub_rn(r, magic) * unit;
+    }
+    const auto four = [&](int i) {
+        return __byte_perm(__byte_perm(b[i], b[i + 1], 0x0040), __byte_perm(b[i + 2], b[i + 3], 0x0040), 0x5410);
+    };
+    return make_uint2(four(0), four(4));
+}
+__device__ __forceinline__ void decode_eight(uint2 c, uint32_t byte, float (&v)[8]) {
+    const float unit = q8_unit(byte);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3))) * unit;
+}
+
+// A thread has 8 values of a row; four neighbours are a block (a row's last block may have idle ones).  I: the type that counts
+// these units.  VEC: every row starts on 16 bytes, so a unit is read as vectors; else value by value (a warp's units lie next to
+// each other, so that the sectors come from L1 after the first touch).  Codes are written 8 at a time in any case.
+template <typename T, typename I, bool VEC>
 __global__ void __launch_bounds__(256) q8_store_kernel(int64_t rows, int64_t inner, const T* __restrict__ x,
                                                        int8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-    const int64_t nb = q8_blocks(inner), pitch = q8_pitch(inner);
-    const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * (blockDim.x >> 5);
-    for (int64_t b = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5); b < rows * nb; b += warps) {
-        const int64_t row = b / nb, at = (b - row * nb) * kQ8Block + lane;
-        const float v = at < inner ? to_f32(x[row * inner + at]) : 0.0f;
-        const uint32_t byte = q8_scale_byte(__reduce_max_sync(~0u, magnitude_bits(v)));
-        if (at < pitch) codes[row * pitch + at] = (int8_t)q8_code(v, byte);
-        if (lane == 0) scales[b] = (uint8_t)byte;
+    const I nb = (I)q8_blocks(inner), per_row = 4 * nb, units = (I)rows * per_row;
+    const int64_t pitch = q8_pitch(inner);
+    const I unit = (I)blockIdx.x * 256 + threadIdx.x;
+    if (unit - (threadIdx.x & 31) >= units) return;           // (a whole warp; units come in fours)
+    const I row = unit / per_row, at = (unit - row * per_row) * 8;
+    const bool ok = unit < units;
+    const T* px = x + (int64_t)row * inner + at;
+    float v[8];
+    if constexpr (VEC) {
+        constexpr int kWords = sizeof(T) / 2, kPer = 16 / sizeof(T);
+        uint4 w[kWords];
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            w[j] = make_uint4(0, 0, 0, 0);
+            if (ok && (int64_t)at + j * kPer < inner) w[j] = __ldg(reinterpret_cast<const uint4*>(px) + j);
+        }
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            const uint32_t q[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(T) == 4) v[4 * j + i] = __uint_as_float(q[i]);
+                else {
+                    v[2 * i] = __uint_as_float(q[i] << 16);
+                    v[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
+                }
+            }
+        }
+    } else {
+        T s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            s[i] = zero_of<T>();
+            if (ok && (int64_t)at + i < inner) s[i] = __ldg(px + i);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_f32(s[i]);
+    }
+    const uint32_t byte = block_scale<4>(v);
+    const uint2 c = encode_eight(v, byte);
+    if (ok && (int64_t)at < pitch) {
+        *reinterpret_cast<uint2*>(codes + (int64_t)row * pitch + at) = c;
+        if (at % kQ8Block == 0) scales[(int64_t)row * nb + at / kQ8Block] = (uint8_t)byte;
     }
 }
 
-template <typename T>
+// ROWS: rows are whole vectors, a thread restores 8 values of one; else it restores 8 values that lie next to each other in the
+// result, whose writes are the ones that have to be whole, from wherever their codes are.
+template <typename T, typename I, bool ROWS>
 __global__ void __launch_bounds__(256) q8_restore_kernel(int64_t rows, int64_t inner, const int8_t* __restrict__ codes,
                                                          const uint8_t* __restrict__ scales, T* __restrict__ x) {
-    const int64_t nb = q8_blocks(inner), pitch = q8_pitch(inner), n = rows * inner;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t row = i / inner, at = i - row * inner;
-        x[i] = from_f32<T>((float)codes[row * pitch + at] * q8_unit(scales[row * nb + at / kQ8Block]));
+    constexpr int kWords = sizeof(T) / 2;
+    const I nb = (I)q8_blocks(inner), total = (I)(rows * inner);
+    const int64_t pitch = q8_pitch(inner);
+    const I first = ((I)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (first >= total) return;
+    I row = first / (I)inner, at = first - row * (I)inner;
+    float v[8];
+    if constexpr (ROWS) {
+        const uint2 c = __ldg(reinterpret_cast<const uint2*>(codes + (int64_t)row * pitch + at));
+        decode_eight(c, __ldg(scales + (int64_t)row * nb + at / kQ8Block), v);
+    } else {
+        int q[8];
+        uint32_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q[i] = 0;
+            b[i] = 1;
+            if (first + i < total) {
+                q[i] = __ldg(codes + (int64_t)row * pitch + at);
+                b[i] = __ldg(scales + (int64_t)row * nb + at / kQ8Block);
+            }
+            if (++at == (I)inner) { at = 0; ++row; }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)q[i] * q8_unit(b[i]);
+    }
+    if (first + 8 <= total) {
+        uint32_t w[4 * kWords];
+#pragma unroll
+        for (int i = 0; i < 4 * kWords; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
+            else {
+                const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&p);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kWords; ++j)
+            reinterpret_cast<uint4*>(x + first)[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (first + i < total) x[first + i] = from_f32<T>(v[i]);
     }
 }
 

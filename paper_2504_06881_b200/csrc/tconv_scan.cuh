@@ -169,38 +169,6 @@ __device__ __forceinline__ void put_eight(T* __restrict__ row, uint32_t at, uint
     }
 }
 
-// ---- 8-bit forms: the four threads of a block of 32 positions are neighbours (a row of one thread is one block) ----
-template <int G> __device__ __forceinline__ uint32_t block_scale(const float (&v)[8]) {
-    uint32_t top = magnitude_bits(v[0]);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = max(top, magnitude_bits(v[i]));
-    if constexpr (G > 1) {
-        top = max(top, __shfl_xor_sync(~0u, top, 1));
-        top = max(top, __shfl_xor_sync(~0u, top, 2));
-    }
-    return q8_scale_byte(top);
-}
-// v becomes the values its codes stand for.  Rounded by adding 1.5 * 2^23, whose unit is 1: the code is the sum's low byte.
-__device__ __forceinline__ uint2 encode_eight(float (&v)[8], uint32_t byte) {
-    const float inv = q8_inverse(byte), unit = q8_unit(byte), magic = 12582912.0f;
-    uint32_t b[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float r = byte == 255u ? magic : __fadd_rn(__fmul_rn(v[i], inv), magic);
-        b[i] = __float_as_uint(r);
-        v[i] = __fsub_rn(r, magic) * unit;
-    }
-    const auto four = [&](int i) {
-        return __byte_perm(__byte_perm(b[i], b[i + 1], 0x0040), __byte_perm(b[i + 2], b[i + 3], 0x0040), 0x5410);
-    };
-    return make_uint2(four(0), four(4));
-}
-__device__ __forceinline__ void decode_eight(uint2 c, uint32_t byte, float (&v)[8]) {
-    const float unit = q8_unit(byte);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3))) * unit;
-}
-
 struct Map {
     float P, B;                      // h -> P h + B
 };

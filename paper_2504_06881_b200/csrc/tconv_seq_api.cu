@@ -14,22 +14,31 @@ constexpr int64_t kMost = (int64_t)1 << 40;     // elements of a tensor
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 template <typename... P> bool all_aligned(P... p) { return (aligned16(p) && ...); }
 
-unsigned blocks_of(int64_t n, int64_t most) { return (unsigned)(n < most ? n : most); }
-
 int check_q8(int64_t rows, int64_t inner, int dtype) {
     if (rows <= 0 || inner <= 0 || (dtype != TCONV_F32 && dtype != TCONV_BF16)) return TCONV_ERR_INVALID_ARG;
-    return rows > kMost / inner ? TCONV_ERR_TOO_LARGE : TCONV_OK;
+    return rows > kMost / inner || rows > ((int64_t)1 << 36) / q8_blocks(inner) ? TCONV_ERR_TOO_LARGE : TCONV_OK;   // (31 bits of blocks)
 }
 
-template <typename T> int q8_store_t(int64_t rows, int64_t inner, const void* x, void* codes, void* scales, cudaStream_t st) {
-    const int64_t nb = rows * q8_blocks(inner);
-    q8_store_kernel<T><<<blocks_of((nb + 7) / 8, 148 * 64), 256, 0, st>>>(rows, inner, (const T*)x, (int8_t*)codes, (uint8_t*)scales);
+// Rows of whole blocks are one long row.  Units and values are counted in 32 bits where that is enough.
+struct Q8Rows { int64_t rows, inner; };
+Q8Rows q8_join(int64_t rows, int64_t inner) { return inner % kQ8Block ? Q8Rows{rows, inner} : Q8Rows{1, rows * inner}; }
+
+template <typename T, typename I> int q8_store_t(Q8Rows q, const void* x, void* codes, void* scales, cudaStream_t st) {
+    const unsigned grid = (unsigned)((q.rows * q8_blocks(q.inner) * 4 + 255) / 256);
+    const auto kern = q.inner % (16 / sizeof(T)) == 0 ? q8_store_kernel<T, I, true> : q8_store_kernel<T, I, false>;
+    kern<<<grid, 256, 0, st>>>(q.rows, q.inner, (const T*)x, (int8_t*)codes, (uint8_t*)scales);
     return launched(1, "q8_store");
 }
-template <typename T> int q8_restore_t(int64_t rows, int64_t inner, const void* codes, const void* scales, void* x, cudaStream_t st) {
-    q8_restore_kernel<T><<<blocks_of((rows * inner + 255) / 256, 148 * 64), 256, 0, st>>>(rows, inner, (const int8_t*)codes,
-                                                                                         (const uint8_t*)scales, (T*)x);
+template <typename T, typename I> int q8_restore_t(Q8Rows q, const void* codes, const void* scales, void* x, cudaStream_t st) {
+    const unsigned grid = (unsigned)(((q.rows * q.inner + 7) / 8 + 255) / 256);
+    const auto kern = q.inner % 8 == 0 ? q8_restore_kernel<T, I, true> : q8_restore_kernel<T, I, false>;
+    kern<<<grid, 256, 0, st>>>(q.rows, q.inner, (const int8_t*)codes, (const uint8_t*)scales, (T*)x);
     return launched(1, "q8_restore");
+}
+template <typename F> int q8_types(Q8Rows q, int dtype, F f) {
+    const bool small = q.rows * (q8_blocks(q.inner) * kQ8Block + 8) < (int64_t)1 << 31;
+    if (dtype == TCONV_F32) return small ? f(float{}, uint32_t{}) : f(float{}, int64_t{});
+    return small ? f(__nv_bfloat16{}, uint32_t{}) : f(__nv_bfloat16{}, int64_t{});
 }
 
 int check_scan(const tconv_scan_desc_t* d, ScanArgs* a, ScanPlan* p) {
@@ -105,22 +114,53 @@ int check_norm(const tconv_norm_desc_t* d, NormArgs* a) {
     return TCONV_OK;
 }
 
+// Calls f with R as a constant: 1, 2, 4, ... 32.
+template <int LEAST, int MOST, typename F> void with_reps(int r, F f) {
+    if constexpr (LEAST <= MOST) {
+        if (r == LEAST) f(std::integral_constant<int, LEAST>{});
+        else with_reps<2 * LEAST, MOST>(r, f);
+    }
+}
+
 template <typename T>
-int norm_fwd_t(const NormArgs& a, const void* x, const void* r, const float* w, const NormOut& o, cudaStream_t st) {
-    if (a.P > 1)
-        norm_fwd_cols_kernel<T><<<(unsigned)((q8_blocks(a.P) * a.N + 3) / 4), 128, 0, st>>>(a, (const T*)x, (const T*)r, w, o);
-    else
-        norm_fwd_rows_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, (const T*)x, (const T*)r, w, o);
+int norm_fwd_t(const NormArgs& a, const NormPlan& p, const void* x_, const void* r_, const float* w, const NormOut& o, cudaStream_t st) {
+    constexpr int V = 16 / sizeof(T);
+    const T *x = (const T*)x_, *r = (const T*)r_;
+    if (!p.held) {
+        if (a.P > 1) norm_fwd_cols_any_kernel<T><<<(unsigned)((q8_blocks(a.P) * a.N + 3) / 4), 128, 0, st>>>(a, x, r, w, o);
+        else norm_fwd_rows_any_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, x, r, w, o);
+    } else if (a.P == 1) {
+        const unsigned grid = (unsigned)((a.N + 3) / 4);
+        if (p.vec) with_reps<1, 32 / V>(p.reps, [&](auto R) { norm_fwd_rows_kernel<T, V, R.value><<<grid, 128, 0, st>>>(a, x, r, w, o); });
+        else with_reps<8, 32>(p.reps, [&](auto R) { norm_fwd_rows_kernel<T, 1, R.value><<<grid, 128, 0, st>>>(a, x, r, w, o); });
+    } else {
+        const int64_t tile = p.vec ? V * p.lp : 32;
+        const unsigned grid = (unsigned)((a.P + tile - 1) / tile * a.N), threads = p.warps * 32;
+        if (!p.vec) with_reps<4, 32>(p.reps, [&](auto R) { norm_fwd_cols_kernel<T, 1, 32, R.value><<<grid, threads, 0, st>>>(a, x, r, w, o); });
+        else with_reps<1, 8>(p.reps, [&](auto R) { norm_fwd_cols_kernel<T, V, kQ8Block / V, R.value><<<grid, threads, 0, st>>>(a, x, r, w, o); });
+    }
     return launched(1, "norm_fwd");
 }
-template <typename T> int norm_bwd_t(const NormArgs& a, const NormIn& k, void* gx, float* gw, cudaStream_t st) {
-    if (a.P > 1)
-        norm_bwd_cols_kernel<T><<<(unsigned)((a.P * a.N + 127) / 128), 128, 0, st>>>(a, k, (T*)gx);
-    else
-        norm_bwd_rows_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, k, (T*)gx);
+template <typename T, bool Q8>
+int norm_bwd_t(const NormArgs& a, const NormPlan& p, const NormIn& k, void* gx_, float* gw, float* part, cudaStream_t st) {
+    constexpr int V = 16 / sizeof(T);
+    T* gx = (T*)gx_;
+    if (!gw) part = nullptr;
+    const unsigned grid = (unsigned)p.blocks, threads = p.warps * 32;
+    if (!p.held) {
+        if (a.P > 1) norm_bwd_cols_any_kernel<T><<<(unsigned)((a.P * a.N + 127) / 128), 128, 0, st>>>(a, k, gx);
+        else norm_bwd_rows_any_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, k, gx);
+    } else if (a.P == 1) {
+        if (p.vec) with_reps<1, 32 / V>(p.reps, [&](auto R) { norm_bwd_rows_kernel<T, V, R.value, Q8><<<grid, 128, 0, st>>>(a, k, gx, part); });
+        else with_reps<8, 32>(p.reps, [&](auto R) { norm_bwd_rows_kernel<T, 1, R.value, Q8><<<grid, 128, 0, st>>>(a, k, gx, part); });
+    } else {
+        if (!p.vec) with_reps<4, 32>(p.reps, [&](auto R) { norm_bwd_cols_kernel<T, 1, 32, R.value, Q8><<<grid, threads, 0, st>>>(a, k, gx, part); });
+        else with_reps<1, 8>(p.reps, [&](auto R) { norm_bwd_cols_kernel<T, V, kQ8Block / V, R.value, Q8><<<grid, threads, 0, st>>>(a, k, gx, part); });
+    }
     const int rc = launched(1, "norm_bwd");
     if (rc || !gw) return rc;
-    norm_bwd_weight_kernel<T><<<(unsigned)a.C, 256, 0, st>>>(a, k, gw);
+    if (p.held) norm_weight_sum_kernel<8><<<(unsigned)((a.C + 31) / 32), 256, 0, st>>>(a.C, p.blocks, part, gw);
+    else norm_bwd_weight_any_kernel<T><<<(unsigned)a.C, 256, 0, st>>>(a, k, gw);
     return launched(1, "norm_bwd");
 }
 
@@ -144,7 +184,8 @@ int tconv_q8_store(int64_t rows, int64_t inner, int dtype, const void* x, void* 
     if (!x || !codes || !scales) return TCONV_ERR_INVALID_ARG;
     if (!all_aligned(x, codes, scales)) return TCONV_ERR_MISALIGNED;
     call_begins();
-    return (dtype == TCONV_F32 ? q8_store_t<float> : q8_store_t<__nv_bfloat16>)(rows, inner, x, codes, scales, (cudaStream_t)stream);
+    const Q8Rows q = q8_join(rows, inner);
+    return q8_types(q, dtype, [&](auto t, auto i) { return q8_store_t<decltype(t), decltype(i)>(q, x, codes, scales, (cudaStream_t)stream); });
 }
 
 int tconv_q8_restore(int64_t rows, int64_t inner, int dtype, const void* codes, const void* scales, void* x, void* stream) {
@@ -153,7 +194,8 @@ int tconv_q8_restore(int64_t rows, int64_t inner, int dtype, const void* codes, 
     if (!x || !codes || !scales) return TCONV_ERR_INVALID_ARG;
     if (!all_aligned(x, codes, scales)) return TCONV_ERR_MISALIGNED;
     call_begins();
-    return (dtype == TCONV_F32 ? q8_restore_t<float> : q8_restore_t<__nv_bfloat16>)(rows, inner, codes, scales, x, (cudaStream_t)stream);
+    const Q8Rows q = q8_join(rows, inner);
+    return q8_types(q, dtype, [&](auto t, auto i) { return q8_restore_t<decltype(t), decltype(i)>(q, codes, scales, x, (cudaStream_t)stream); });
 }
 
 size_t tconv_scan_states_bytes(const tconv_scan_desc_t* desc) {
@@ -220,7 +262,12 @@ int tconv_scan_backward(const tconv_scan_desc_t* desc, const void* x, const void
     return scan_any<kBwd>(a, p, io, desc->dtype, kept, vec, (cudaStream_t)stream);
 }
 
-size_t tconv_norm_workspace_bytes(const tconv_norm_desc_t*) { return 0; }
+size_t tconv_norm_workspace_bytes(const tconv_norm_desc_t* desc) {
+    NormArgs a;
+    if (check_norm(desc, &a)) return 0;
+    const NormPlan p = plan_norm(a, desc->dtype);
+    return p.held ? (size_t)p.blocks * a.C * sizeof(float) : 0;
+}
 
 int tconv_norm_forward(const tconv_norm_desc_t* desc, const void* x, const void* residual, const float* weight, void* sum, void* y,
                        float* rstd, void* y_codes, void* y_scales, void* s_codes, void* s_scales, void* stream) {
@@ -232,7 +279,7 @@ int tconv_norm_forward(const tconv_norm_desc_t* desc, const void* x, const void*
     if (!all_aligned(x, residual, weight, sum, y, rstd, y_codes, y_scales, s_codes, s_scales)) return TCONV_ERR_MISALIGNED;
     const NormOut o{sum, y, rstd, (int8_t*)y_codes, (uint8_t*)y_scales, (int8_t*)s_codes, (uint8_t*)s_scales};
     call_begins();
-    return (desc->dtype == TCONV_F32 ? norm_fwd_t<float> : norm_fwd_t<__nv_bfloat16>)(a, x, residual, weight, o, (cudaStream_t)stream);
+    return (desc->dtype == TCONV_F32 ? norm_fwd_t<float> : norm_fwd_t<__nv_bfloat16>)(a, plan_norm(a, desc->dtype), x, residual, weight, o, (cudaStream_t)stream);
 }
 
 int tconv_norm_backward(const tconv_norm_desc_t* desc, const void* s, const void* s_codes, const void* s_scales, const float* rstd,
@@ -243,10 +290,13 @@ int tconv_norm_backward(const tconv_norm_desc_t* desc, const void* s, const void
     if (rc) return rc;
     if (!s_codes != !s_scales || !s == !s_codes || !rstd || !weight || !grad_y || !grad_x) return TCONV_ERR_INVALID_ARG;
     if (!all_aligned(s, s_codes, s_scales, rstd, weight, grad_y, grad_sum, grad_x, grad_weight, workspace)) return TCONV_ERR_MISALIGNED;
-    if (workspace_bytes < tconv_norm_workspace_bytes(desc)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = grad_weight ? tconv_norm_workspace_bytes(desc) : 0;
+    if (workspace_bytes < need || (need && !workspace)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
     const NormIn k{s, (const int8_t*)s_codes, (const uint8_t*)s_scales, rstd, weight, grad_y, grad_sum};
     call_begins();
-    return (desc->dtype == TCONV_F32 ? norm_bwd_t<float> : norm_bwd_t<__nv_bfloat16>)(a, k, grad_x, grad_weight, (cudaStream_t)stream);
+    const auto run = desc->dtype == TCONV_F32 ? (s ? norm_bwd_t<float, false> : norm_bwd_t<float, true>)
+                                              : (s ? norm_bwd_t<__nv_bfloat16, false> : norm_bwd_t<__nv_bfloat16, true>);
+    return run(a, plan_norm(a, desc->dtype), k, grad_x, grad_weight, (float*)workspace, (cudaStream_t)stream);
 }
 
 }  // extern "C"
