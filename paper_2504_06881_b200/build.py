@@ -35,9 +35,9 @@ def _newest_source() -> float:
     return max(f.stat().st_mtime for f in files)
 
 
-def _nvcc_base(verbose: bool):
+def _nvcc_base(verbose: bool, std: str = "c++17"):
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", f"-std={std}", "-lineinfo",
            "-Xcompiler", "-fPIC", "-I", str(ROOT / "include"), "-I", str(CSRC)]
     if verbose:
         cmd += ["-Xptxas", "-v"]
@@ -66,7 +66,7 @@ def _compile(job):
     if src.suffix == ".cpp":
         cmd = [HOST_CXX] + _torch_flags()[0] + ["-c", str(src), "-o", str(obj)]
     else:
-        cmd = _nvcc_base(verbose) + defs + ["-c", str(src), "-o", str(obj)]
+        cmd = _nvcc_base(verbose, "c++20" if src.stem.startswith("tconv_seq") else "c++17") + defs + ["-c", str(src), "-o", str(obj)]
     r = subprocess.run(cmd, capture_output=True, text=True)
     return obj, r.returncode, r.stdout + r.stderr
 

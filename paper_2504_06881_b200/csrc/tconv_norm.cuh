@@ -7,6 +7,8 @@
 #pragma once
 #include "tconv_q8.cuh"
 
+#include <type_traits>
+
 namespace tconv {
 
 struct NormArgs {
@@ -101,10 +103,9 @@ template <typename T, int V> __device__ __forceinline__ Some<T, V> gather(const 
     return s;
 }
 
-// Stores V values at place `at` of a row of an 8-bit form; the 32 / V lanes of a block are neighbours, and every lane of the warp
-// calls.  ok: the row exists.
-template <int V>
-__device__ __forceinline__ void q8_put_some(const float (&v)[V], bool ok, int64_t row, int64_t at, int64_t inner, int8_t* codes, uint8_t* scales) {
+// Stores V values of an 8-bit form: codes to `to`, and at a block's first value the scale byte to `scale`; the 32 / V lanes of a block
+// are neighbours, and every lane of the warp calls.  ok: the values are there to be stored.
+template <int V> __device__ __forceinline__ void q8_put_some(const float (&v)[V], bool ok, int8_t* to, bool head, uint8_t* scale) {
     uint32_t top = magnitude_bits(v[0]);
 #pragma unroll
     for (int i = 1; i < V; ++i) top = max(top, magnitude_bits(v[i]));
@@ -113,13 +114,14 @@ __device__ __forceinline__ void q8_put_some(const float (&v)[V], bool ok, int64_
 #pragma unroll
         for (int d = 1; d < kQ8Block / V; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
     const uint32_t byte = q8_scale_byte(top);
-    if (!ok || at >= q8_pitch(inner)) return;
-    int8_t* to = codes + row * q8_pitch(inner) + at;
+    if (!ok) return;
     uint32_t b[V];
     const float inv = q8_inverse(byte);
 #pragma unroll
-    for (int i = 0; i < V; ++i)      // (1.5 * 2^23 has unit 1: the code is the sum's low byte)
-        b[i] = byte == 255u ? 0u : __float_as_uint(__fadd_rn(__fmul_rn(v[i], inv), 12582912.0f));
+    for (int i = 0; i < V; ++i) {    // (1.5 * 2^23 has unit 1: the code is the sum's low byte)
+        const float t = __fadd_rn(__fmul_rn(v[i], inv), 12582912.0f);
+        b[i] = byte == 255u ? 0u : __float_as_uint(t);
+    }
     if constexpr (V == 1) *to = (int8_t)b[0];
     else {
         uint32_t w[V / 4];
@@ -129,27 +131,26 @@ __device__ __forceinline__ void q8_put_some(const float (&v)[V], bool ok, int64_
         if constexpr (V == 4) *reinterpret_cast<uint32_t*>(to) = w[0];
         else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
     }
-    if (at % kQ8Block == 0 && at < inner) scales[row * q8_blocks(inner) + at / kQ8Block] = (uint8_t)byte;
+    if (head) *scale = (uint8_t)byte;
 }
 
 // The stream's V values for the backward pass: itself, or its codes and their unit.
 template <typename T, int V, bool Q8> struct Kept {
     Some<T, V> s;
-    __device__ __forceinline__ void load(const NormIn& k, int64_t row, int64_t at, int64_t inner) { s = load_some<T, V>(k.s, row * inner + at); }
+    __device__ __forceinline__ void load(const T* p, const int8_t*, const uint8_t*) { s = load_some<T, V>(p, 0); }
     __device__ __forceinline__ void none() { s = none_of<T, V>(); }
     __device__ __forceinline__ void values(float (&v)[V]) const { spread<T, V>(s, v); }
 };
 template <typename T, int V> struct Kept<T, V, true> {
     uint32_t w[V == 8 ? 2 : 1], byte;
-    __device__ __forceinline__ void load(const NormIn& k, int64_t row, int64_t at, int64_t inner) {
-        const int8_t* p = k.sc + row * q8_pitch(inner) + at;
+    __device__ __forceinline__ void load(const T*, const int8_t* c, const uint8_t* scale) {
         if constexpr (V == 8) {
-            const uint2 c = __ldg(reinterpret_cast<const uint2*>(p));
-            w[0] = c.x;
-            w[1] = c.y;
-        } else if constexpr (V == 4) w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-        else w[0] = (uint8_t)__ldg(p);
-        byte = __ldg(k.ss + row * q8_blocks(inner) + at / kQ8Block);
+            const uint2 q = __ldg(reinterpret_cast<const uint2*>(c));
+            w[0] = q.x;
+            w[1] = q.y;
+        } else if constexpr (V == 4) w[0] = __ldg(reinterpret_cast<const uint32_t*>(c));
+        else w[0] = (uint8_t)__ldg(c);
+        byte = __ldg(scale);
     }
     __device__ __forceinline__ void none() {
         w[0] = 0;
@@ -163,31 +164,28 @@ template <typename T, int V> struct Kept<T, V, true> {
     }
 };
 
-// P > 1.  A warp has LP lanes of V positions each and 32 / LP channels at a time, a thread R channels.
-template <int V, int LP> struct Cols {
-    static constexpr int kTile = V * LP;       // positions of a block
-    static_assert(kTile % kQ8Block == 0, "an 8-bit block is a warp's affair");
-    int lp, cg, cs;                            // lane's place among positions; first channel, channels at a time
-    __device__ __forceinline__ Cols() {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        lp = lane % LP;
-        cg = warp * (32 / LP) + lane / LP;
-        cs = (blockDim.x >> 5) * (32 / LP);
-    }
-    // Sums v over the block's threads that share positions, then lets `last` turn each position's sum into what all of them get.
-    template <typename F> __device__ __forceinline__ void sum(float (&v)[V], float (*part)[kTile], float* total, F last) {
+// P > 1.  A block has WARPS warps and 32 positions of one image, an 8-bit block of every channel; a warp has 32 / V lanes of V
+// positions each and V channels at a time, a thread R channels.  Offsets inside an image are 32 bits wide.
+template <int V, int WARPS> struct Cols {
+    static constexpr int kLanes = kQ8Block / V, kStep = WARPS * V;     // lanes along positions; channels at a time
+    const int lp, c0;                                                   // the lane's place among positions; its first channel
+    __device__ __forceinline__ Cols() : lp(threadIdx.x % kLanes), c0(threadIdx.x / kLanes) {}
+    __device__ __forceinline__ int channels(int C) const { return c0 < C ? (C - c0 + kStep - 1) / kStep : 0; }
+    // Sums v over the threads that share positions; `last` turns a position's sum into what all of them get.
+    template <typename F> __device__ __forceinline__ void sum(float (&v)[V], float (*part)[kQ8Block], float* total, F last) const {
 #pragma unroll
-        for (int d = LP; d < 32; d <<= 1)
+        for (int d = kLanes; d < 32; d <<= 1)
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] += __shfl_xor_sync(~0u, v[i], d);
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-        if (lane < LP)
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        if (lane < kLanes)
 #pragma unroll
-            for (int i = 0; i < V; ++i) part[warp][lp * V + i] = v[i];
+            for (int i = 0; i < V; ++i) part[warp][lane * V + i] = v[i];
         __syncthreads();
-        if (threadIdx.x < kTile) {
+        if (threadIdx.x < kQ8Block) {
             float t = 0.0f;
-            for (int w = 0; w < warps; ++w) t += part[w][threadIdx.x];
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) t += part[w][threadIdx.x];
             total[threadIdx.x] = last(t, threadIdx.x);
         }
         __syncthreads();
@@ -196,42 +194,52 @@ template <int V, int LP> struct Cols {
     }
 };
 
-template <typename T, int V, int LP, int R>
-__global__ void __launch_bounds__(512) norm_fwd_cols_kernel(const __grid_constant__ NormArgs a, const T* __restrict__ x,
+// Blocks of the backward kernel that an SM holds: 128 registers a thread.
+constexpr int norm_resident(int warps) { return 16 / warps; }
+
+// RES: with a residual; Q8: some output in 8 bits.
+template <typename T, int V, int WARPS, int R, bool RES, bool Q8>
+__global__ void __launch_bounds__(WARPS * 32) norm_fwd_cols_kernel(const __grid_constant__ NormArgs a, const T* __restrict__ x,
         const T* __restrict__ r, const float* __restrict__ w, const __grid_constant__ NormOut o) {
-    using B = Cols<V, LP>;
-    __shared__ float part[16][B::kTile], total[B::kTile];
-    B b;
-    const int64_t tiles = (a.P + B::kTile - 1) / B::kTile, n = blockIdx.x / tiles, p0 = (blockIdx.x - n * tiles) * B::kTile, p = p0 + b.lp * V;
-    const bool in = p < a.P;
+    __shared__ float part[WARPS][kQ8Block], total[kQ8Block];
+    const Cols<V, WARPS> b;
+    const uint32_t P = (uint32_t)a.P, tiles = (P + kQ8Block - 1) / kQ8Block, pitch = (uint32_t)q8_pitch(a.P);
+    const uint32_t n = blockIdx.x / tiles, p0 = (blockIdx.x - n * tiles) * kQ8Block, p = p0 + b.lp * V;
+    const int have = b.channels(a.C), live = p < P ? have : 0;          // channels of this thread; with positions in the image
+    const int64_t image = (int64_t)n * a.C * P;
+    const uint32_t at = b.c0 * P + p, step = b.kStep * P;
+    x += image;
     Some<T, V> s[R];
-    float sq[V];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-        const int c = b.cg + j * b.cs;
         s[j] = none_of<T, V>();
-        if (in && c < a.C) s[j] = load_some<T, V>(x, (n * a.C + c) * a.P + p);
+        if (j < live) s[j] = load_some<T, V>(x, at + j * step);
     }
-    if (r) {
+    if constexpr (RES) {
+        r += image;
+        T* sum = (T*)o.sum + image;
         Some<T, V> t[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int c = b.cg + j * b.cs;
             t[j] = none_of<T, V>();
-            if (in && c < a.C) t[j] = load_some<T, V>(r, (n * a.C + c) * a.P + p);
+            if (j < live) t[j] = load_some<T, V>(r, at + j * step);
         }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int c = b.cg + j * b.cs;
             float u[V], v[V];
             spread<T, V>(s[j], u);
             spread<T, V>(t[j], v);
 #pragma unroll
             for (int i = 0; i < V; ++i) u[i] += v[i];
             s[j] = gather<T, V>(u);
-            if (in && c < a.C) store_some<T, V>(o.sum, (n * a.C + c) * a.P + p, s[j]);
+            if (j < live) store_some<T, V>(sum, at + j * step, s[j]);
         }
     }
+    const auto put = [&](const float (&v)[V], int j, int8_t* codes, uint8_t* scales) {
+        const int64_t row = (int64_t)n * a.C + b.c0 + j * b.kStep;
+        q8_put_some<V>(v, j < have && p < pitch, codes + row * pitch + p, b.lp == 0, scales + row * tiles + p0 / kQ8Block);
+    };
+    float sq[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sq[i] = 0.0f;
 #pragma unroll
@@ -240,71 +248,84 @@ __global__ void __launch_bounds__(512) norm_fwd_cols_kernel(const __grid_constan
         spread<T, V>(s[j], v);
 #pragma unroll
         for (int i = 0; i < V; ++i) sq[i] = fmaf(v[i], v[i], sq[i]);
-        if (o.sc) {
-            const int c = b.cg + j * b.cs;
-            q8_put_some<V>(v, c < a.C, n * a.C + c, p, a.P, o.sc, o.ss);
-        }
+        if constexpr (Q8)
+            if (o.sc) put(v, j, o.sc, o.ss);
     }
-    b.sum(sq, part, total, [&](float t, int i) {
+    b.sum(sq, part, total, [&](float t, uint32_t i) {
         const float rstd = 1.0f / sqrtf(t / (float)a.C + a.eps);
-        if (o.rstd && p0 + i < a.P) o.rstd[n * a.P + p0 + i] = rstd;
+        if (o.rstd && p0 + i < P) o.rstd[(int64_t)n * P + p0 + i] = rstd;
         return rstd;
     });
+    T* y = (T*)o.y + image;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-        const int c = b.cg + j * b.cs;
-        const float wc = c < a.C ? __ldg(w + c) : 0.0f;
+        const float wc = j < have ? __ldg(w + b.c0 + j * b.kStep) : 0.0f;
         float v[V];
         spread<T, V>(s[j], v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = in ? v[i] * sq[i] * wc : 0.0f;
-        if (o.y && in && c < a.C) store_some<T, V>(o.y, (n * a.C + c) * a.P + p, gather<T, V>(v));
-        if (o.yc) q8_put_some<V>(v, c < a.C, n * a.C + c, p, a.P, o.yc, o.ys);
+        for (int i = 0; i < V; ++i) v[i] = v[i] * sq[i] * wc;
+        if constexpr (Q8) {
+            if (o.y && j < live) store_some<T, V>(y, at + j * step, gather<T, V>(v));
+            if (o.yc) {
+                if (j >= live)       // (a row's end, where 0 * NaN must not poison the block)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[i] = 0.0f;
+                put(v, j, o.yc, o.ys);
+            }
+        } else if (j < live) store_some<T, V>(y, at + j * step, gather<T, V>(v));
     }
 }
 
-// part: [gridDim.x][C], this block's sums of grad_weight (NULL: not wanted).
-template <typename T, int V, int LP, int R, bool Q8>
-__global__ void __launch_bounds__(512) norm_bwd_cols_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
-                                                            T* __restrict__ gx, float* __restrict__ gw_part) {
-    using B = Cols<V, LP>;
-    __shared__ float part[16][B::kTile], total[B::kTile];
-    B b;
-    const int64_t tiles = (a.P + B::kTile - 1) / B::kTile, all = tiles * a.N;
+// gw_part: [gridDim.x][C], each block's sums of grad_weight (NULL: not wanted).  RES: the stream has a gradient of its own.
+template <typename T, int V, int WARPS, int R, bool RES, bool Q8>
+__global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_cols_kernel(
+        const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k, T* __restrict__ gx, float* __restrict__ gw_part) {
+    __shared__ float part[WARPS][kQ8Block], total[kQ8Block];
+    const Cols<V, WARPS> b;
+    const uint32_t P = (uint32_t)a.P, tiles = (P + kQ8Block - 1) / kQ8Block, all = tiles * a.N, pitch = (uint32_t)q8_pitch(a.P);
+    const uint32_t step = b.kStep * P;
+    const int have = b.channels(a.C);
     float gw[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) gw[j] = 0.0f;
-    for (int64_t tile = blockIdx.x; tile < all; tile += gridDim.x) {
-        const int64_t n = tile / tiles, p = (tile - n * tiles) * B::kTile + b.lp * V;
-        const bool in = p < a.P;
+    for (uint32_t tile = blockIdx.x; tile < all; tile += gridDim.x) {
+        const uint32_t n = tile / tiles, p0 = (tile - n * tiles) * kQ8Block, p = p0 + b.lp * V;
+        const int live = p < P ? have : 0;
+        const int64_t image = (int64_t)n * a.C * P, row0 = (int64_t)n * a.C + b.c0;
+        const uint32_t at = b.c0 * P + p;
+        const T *ps = (const T*)k.s + image, *py = (const T*)k.gy + image, *pg = (const T*)k.gs + image;
         Kept<T, V, Q8> s[R];
-        Some<T, V> dy[R];
+        Some<T, V> dy[R], ds[RES ? R : 1];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int c = b.cg + j * b.cs;
             s[j].none();
             dy[j] = none_of<T, V>();
-            if (in && c < a.C) {
-                s[j].load(k, n * a.C + c, p, a.P);
-                dy[j] = load_some<T, V>(k.gy, (n * a.C + c) * a.P + p);
+            if (j < live) {
+                const int64_t row = row0 + j * b.kStep;
+                s[j].load(ps + (at + j * step), k.sc + row * pitch + p, k.ss + row * tiles + p0 / kQ8Block);
+                dy[j] = load_some<T, V>(py, at + j * step);
             }
         }
         float rstd[V], m[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) rstd[i] = m[i] = 0.0f;
-        if (in) {
-            if constexpr (V == 1) rstd[0] = __ldg(k.rstd + n * a.P + p);
+        if (p < P) {
+            const float* pr = k.rstd + (int64_t)n * P + p;
+            if constexpr (V == 1) rstd[0] = __ldg(pr);
             else
 #pragma unroll
                 for (int i = 0; i < V; i += 4) {
-                    const float4 q = __ldg(reinterpret_cast<const float4*>(k.rstd + n * a.P + p + i));
+                    const float4 q = __ldg(reinterpret_cast<const float4*>(pr + i));
                     rstd[i] = q.x; rstd[i + 1] = q.y; rstd[i + 2] = q.z; rstd[i + 3] = q.w;
                 }
         }
+        if constexpr (RES && V > 1)
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+                if (j < live) ds[j] = load_some<T, V>(pg, at + j * step);
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int c = b.cg + j * b.cs;
-            const float wc = c < a.C ? __ldg(k.w + c) : 0.0f;
+            const float wc = j < have ? __ldg(k.w + b.c0 + j * b.kStep) : 0.0f;
             float v[V], d[V];
             s[j].values(v);
             spread<T, V>(dy[j], d);
@@ -316,32 +337,32 @@ __global__ void __launch_bounds__(512) norm_bwd_cols_kernel(const __grid_constan
             }
         }
         b.sum(m, part, total, [&](float t, int) { return t / (float)a.C; });
+        T* po = gx + image;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int c = b.cg + j * b.cs;
-            if (!in || c >= a.C) continue;
-            const float wc = __ldg(k.w + c);
-            const int64_t at = (n * a.C + c) * a.P + p;
-            float v[V], d[V], e[V];
+            if (j >= live) continue;
+            const float wc = __ldg(k.w + b.c0 + j * b.kStep);
+            float v[V], d[V];
             s[j].values(v);
             spread<T, V>(dy[j], d);
 #pragma unroll
             for (int i = 0; i < V; ++i) d[i] = rstd[i] * (wc * d[i] - v[i] * rstd[i] * m[i]);
-            if (k.gs) {
-                spread<T, V>(load_some<T, V>(k.gs, at), e);
+            if constexpr (RES) {
+                float e[V];
+                if constexpr (V > 1) spread<T, V>(ds[j], e);
+                else spread<T, V>(load_some<T, V>(pg, at + j * step), e);
 #pragma unroll
                 for (int i = 0; i < V; ++i) d[i] += e[i];
             }
-            store_some<T, V>(gx, at, gather<T, V>(d));
+            store_some<T, V>(po, at + j * step, gather<T, V>(d));
         }
     }
     if (!gw_part) return;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
 #pragma unroll
-        for (int d = 1; d < LP; d <<= 1) gw[j] += __shfl_xor_sync(~0u, gw[j], d);
-        const int c = b.cg + j * b.cs;
-        if (b.lp == 0 && c < a.C) gw_part[(int64_t)blockIdx.x * a.C + c] = gw[j];
+        for (int d = 1; d < b.kLanes; d <<= 1) gw[j] += __shfl_xor_sync(~0u, gw[j], d);
+        if (b.lp == 0 && j < have) gw_part[(int64_t)blockIdx.x * a.C + b.c0 + j * b.kStep] = gw[j];
     }
 }
 
@@ -352,6 +373,10 @@ __global__ void __launch_bounds__(128) norm_fwd_rows_kernel(const __grid_constan
     const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (n >= a.N) return;
     const int lane = threadIdx.x & 31;
+    const int pitch = (int)q8_pitch(a.C), nb = (int)q8_blocks(a.C);
+    const auto put = [&](const float (&v)[V], int c, int8_t* codes, uint8_t* scales) {
+        q8_put_some<V>(v, c < pitch, codes + n * pitch + c, c % kQ8Block == 0 && c < a.C, scales + n * nb + c / kQ8Block);
+    };
     Some<T, V> s[R];
     float sq = 0.0f;
 #pragma unroll
@@ -378,7 +403,7 @@ __global__ void __launch_bounds__(128) norm_fwd_rows_kernel(const __grid_constan
         spread<T, V>(s[j], v);
 #pragma unroll
         for (int i = 0; i < V; ++i) sq = fmaf(v[i], v[i], sq);
-        if (o.sc) q8_put_some<V>(v, true, n, c, a.C, o.sc, o.ss);
+        if (o.sc) put(v, c, o.sc, o.ss);
     }
     const float rstd = 1.0f / sqrtf(warp_sum(sq) / (float)a.C + a.eps);
     if (o.rstd && lane == 0) o.rstd[n] = rstd;
@@ -390,7 +415,7 @@ __global__ void __launch_bounds__(128) norm_fwd_rows_kernel(const __grid_constan
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = c < a.C ? v[i] * rstd * __ldg(w + c + i) : 0.0f;
         if (o.y && c < a.C) store_some<T, V>(o.y, n * a.C + c, gather<T, V>(v));
-        if (o.yc) q8_put_some<V>(v, true, n, c, a.C, o.yc, o.ys);
+        if (o.yc) put(v, c, o.yc, o.ys);
     }
 }
 
@@ -398,7 +423,7 @@ template <typename T, int V, int R, bool Q8>
 __global__ void __launch_bounds__(128) norm_bwd_rows_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
                                                             T* __restrict__ gx, float* __restrict__ gw_part) {
     __shared__ float sums[4][32 * V * R];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = (int)q8_pitch(a.C), nb = (int)q8_blocks(a.C);
     float gw[R][V];
 #pragma unroll
     for (int j = 0; j < R; ++j)
@@ -415,7 +440,7 @@ __global__ void __launch_bounds__(128) norm_bwd_rows_kernel(const __grid_constan
             s[j].none();
             dy[j] = none_of<T, V>();
             if (c < a.C) {
-                s[j].load(k, n, c, a.C);
+                s[j].load((const T*)k.s + n * a.C + c, k.sc + n * pitch + c, k.ss + n * nb + c / kQ8Block);
                 dy[j] = load_some<T, V>(k.gy, n * a.C + c);
             }
         }
@@ -476,38 +501,59 @@ __global__ void __launch_bounds__(256) norm_weight_sum_kernel(int C, int blocks,
 
 // What a layer's kernels look like.
 struct NormPlan {
-    bool held;                       // a block holds all channels of its positions
     bool vec;                        // 16 bytes at a time
-    int warps, lp, reps, blocks;     // warps of a block, lanes along positions, channels of a thread, blocks of the backward pass
+    int form;                        // which of the kernels with all channels in registers; -1: none holds that many
+    int blocks;                      // of the backward pass
 };
+
+// The kernels with P > 1, by V, warps and channels of a thread, from the smallest that holds all channels on.
+template <typename F> void with_cols(std::integral_constant<int, 8>, int form, F f) {
+    if (form == 0) f.template operator()<8, 4, 2>();
+    else if (form == 1) f.template operator()<8, 4, 4>();
+    else if (form == 2) f.template operator()<8, 8, 4>();
+    else if (form == 3) f.template operator()<8, 16, 4>();
+    else f.template operator()<8, 16, 8>();
+}
+template <typename F> void with_cols(std::integral_constant<int, 4>, int form, F f) {
+    if (form == 0) f.template operator()<4, 4, 2>();
+    else if (form == 1) f.template operator()<4, 4, 4>();
+    else if (form == 2) f.template operator()<4, 8, 4>();
+    else if (form == 3) f.template operator()<4, 16, 4>();
+    else f.template operator()<4, 16, 8>();
+}
+template <typename F> void with_cols(std::integral_constant<int, 1>, int form, F f) {
+    if (form == 0) f.template operator()<1, 4, 8>();
+    else if (form == 1) f.template operator()<1, 4, 16>();
+    else if (form == 2) f.template operator()<1, 8, 16>();
+    else if (form == 3) f.template operator()<1, 16, 16>();
+    else f.template operator()<1, 16, 32>();
+}
 
 inline NormPlan plan_norm(const NormArgs& a, int dtype) {
     const int V = dtype == TCONV_F32 ? 4 : 8;
     NormPlan p{};
     p.vec = (a.P > 1 ? a.P : a.C) % V == 0;
-    const auto reps = [](int need, int least, int most) {
-        int r = least;
-        while (r < need) r *= 2;
-        return r <= most ? r : 0;
-    };
+    p.form = -1;
     if (a.P == 1) {
-        p.warps = 4;
-        p.reps = p.vec ? reps((a.C + 32 * V - 1) / (32 * V), 1, 32 / V) : reps((a.C + 31) / 32, 8, 32);
+        const int least = p.vec ? 32 * V : 256;
+        for (int k = 0; p.form < 0 && (least << k) <= 1024; ++k)
+            if (a.C <= least << k) p.form = k;
         p.blocks = (a.N + 3) / 4 < 148 * 2 ? (a.N + 3) / 4 : 148 * 2;
     } else {
-        if (p.vec) {
-            p.lp = kQ8Block / V;
-            p.warps = a.C <= 128 ? 8 : 16;
-            p.reps = reps((a.C + p.warps * (32 / p.lp) - 1) / (p.warps * (32 / p.lp)), 1, 8);
-        } else {
-            p.lp = 32;
-            p.warps = a.C <= 128 ? 4 : a.C <= 256 ? 8 : 16;
-            p.reps = reps((a.C + p.warps - 1) / p.warps, 4, 32);
-        }
-        const int64_t tile = p.vec ? V * p.lp : 32, tiles = (a.P + tile - 1) / tile * a.N, most = 148 * (16 / p.warps);
-        p.blocks = (int)(tiles < most ? tiles : most);
+        if ((int64_t)a.C * a.P >= (int64_t)1 << 30) return p;       // (offsets inside an image: 32 bits, in bytes)
+        const auto take = [&](auto v) {
+            for (int k = 4; k >= 0; --k)
+                with_cols(v, k, [&]<int VV, int WARPS, int R>() {
+                    if (a.C > VV * WARPS * R) return;
+                    p.form = k;
+                    const int64_t tiles = q8_blocks(a.P) * a.N, most = 148 * norm_resident(WARPS);
+                    p.blocks = (int)(tiles < most ? tiles : most);
+                });
+        };
+        if (!p.vec) take(std::integral_constant<int, 1>{});
+        else if (V == 4) take(std::integral_constant<int, 4>{});
+        else take(std::integral_constant<int, 8>{});
     }
-    p.held = p.reps > 0;
     return p;
 }
 

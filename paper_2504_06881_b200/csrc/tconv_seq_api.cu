@@ -114,52 +114,64 @@ int check_norm(const tconv_norm_desc_t* d, NormArgs* a) {
     return TCONV_OK;
 }
 
-// Calls f with R as a constant: 1, 2, 4, ... 32.
-template <int LEAST, int MOST, typename F> void with_reps(int r, F f) {
+// Calls f with R as a constant: LEAST << k.
+template <int LEAST, int MOST, typename F> void with_reps(int k, F f) {
     if constexpr (LEAST <= MOST) {
-        if (r == LEAST) f(std::integral_constant<int, LEAST>{});
-        else with_reps<2 * LEAST, MOST>(r, f);
+        if (k == 0) f.template operator()<LEAST>();
+        else with_reps<2 * LEAST, MOST>(k - 1, f);
     }
+}
+template <typename F> void with_flags(bool p, bool q, F f) {
+    if (p) q ? f.template operator()<true, true>() : f.template operator()<true, false>();
+    else q ? f.template operator()<false, true>() : f.template operator()<false, false>();
 }
 
 template <typename T>
 int norm_fwd_t(const NormArgs& a, const NormPlan& p, const void* x_, const void* r_, const float* w, const NormOut& o, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
     const T *x = (const T*)x_, *r = (const T*)r_;
-    if (!p.held) {
+    if (p.form < 0) {
         if (a.P > 1) norm_fwd_cols_any_kernel<T><<<(unsigned)((q8_blocks(a.P) * a.N + 3) / 4), 128, 0, st>>>(a, x, r, w, o);
         else norm_fwd_rows_any_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, x, r, w, o);
     } else if (a.P == 1) {
         const unsigned grid = (unsigned)((a.N + 3) / 4);
-        if (p.vec) with_reps<1, 32 / V>(p.reps, [&](auto R) { norm_fwd_rows_kernel<T, V, R.value><<<grid, 128, 0, st>>>(a, x, r, w, o); });
-        else with_reps<8, 32>(p.reps, [&](auto R) { norm_fwd_rows_kernel<T, 1, R.value><<<grid, 128, 0, st>>>(a, x, r, w, o); });
+        if (p.vec) with_reps<1, 32 / V>(p.form, [&]<int R>() { norm_fwd_rows_kernel<T, V, R><<<grid, 128, 0, st>>>(a, x, r, w, o); });
+        else with_reps<8, 32>(p.form, [&]<int R>() { norm_fwd_rows_kernel<T, 1, R><<<grid, 128, 0, st>>>(a, x, r, w, o); });
     } else {
-        const int64_t tile = p.vec ? V * p.lp : 32;
-        const unsigned grid = (unsigned)((a.P + tile - 1) / tile * a.N), threads = p.warps * 32;
-        if (!p.vec) with_reps<4, 32>(p.reps, [&](auto R) { norm_fwd_cols_kernel<T, 1, 32, R.value><<<grid, threads, 0, st>>>(a, x, r, w, o); });
-        else with_reps<1, 8>(p.reps, [&](auto R) { norm_fwd_cols_kernel<T, V, kQ8Block / V, R.value><<<grid, threads, 0, st>>>(a, x, r, w, o); });
+        const unsigned grid = (unsigned)(q8_blocks(a.P) * a.N);
+        const auto go = [&]<int VV, int WARPS, int R>() {
+            with_flags(r, o.yc || o.sc, [&]<bool RES, bool Q8>() { norm_fwd_cols_kernel<T, VV, WARPS, R, RES, Q8><<<grid, WARPS * 32, 0, st>>>(a, x, r, w, o); });
+        };
+        if (p.vec) with_cols(std::integral_constant<int, V>{}, p.form, go);
+        else with_cols(std::integral_constant<int, 1>{}, p.form, go);
     }
     return launched(1, "norm_fwd");
 }
-template <typename T, bool Q8>
-int norm_bwd_t(const NormArgs& a, const NormPlan& p, const NormIn& k, void* gx_, float* gw, float* part, cudaStream_t st) {
+template <typename T> int norm_bwd_t(const NormArgs& a, const NormPlan& p, const NormIn& k, void* gx_, float* gw, float* part, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
     T* gx = (T*)gx_;
     if (!gw) part = nullptr;
-    const unsigned grid = (unsigned)p.blocks, threads = p.warps * 32;
-    if (!p.held) {
+    const unsigned grid = (unsigned)p.blocks;
+    if (p.form < 0) {
         if (a.P > 1) norm_bwd_cols_any_kernel<T><<<(unsigned)((a.P * a.N + 127) / 128), 128, 0, st>>>(a, k, gx);
         else norm_bwd_rows_any_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, k, gx);
     } else if (a.P == 1) {
-        if (p.vec) with_reps<1, 32 / V>(p.reps, [&](auto R) { norm_bwd_rows_kernel<T, V, R.value, Q8><<<grid, 128, 0, st>>>(a, k, gx, part); });
-        else with_reps<8, 32>(p.reps, [&](auto R) { norm_bwd_rows_kernel<T, 1, R.value, Q8><<<grid, 128, 0, st>>>(a, k, gx, part); });
+        const auto go = [&]<int VV, int R>() {
+            if (k.s) norm_bwd_rows_kernel<T, VV, R, false><<<grid, 128, 0, st>>>(a, k, gx, part);
+            else norm_bwd_rows_kernel<T, VV, R, true><<<grid, 128, 0, st>>>(a, k, gx, part);
+        };
+        if (p.vec) with_reps<1, 32 / V>(p.form, [&]<int R>() { go.template operator()<V, R>(); });
+        else with_reps<8, 32>(p.form, [&]<int R>() { go.template operator()<1, R>(); });
     } else {
-        if (!p.vec) with_reps<4, 32>(p.reps, [&](auto R) { norm_bwd_cols_kernel<T, 1, 32, R.value, Q8><<<grid, threads, 0, st>>>(a, k, gx, part); });
-        else with_reps<1, 8>(p.reps, [&](auto R) { norm_bwd_cols_kernel<T, V, kQ8Block / V, R.value, Q8><<<grid, threads, 0, st>>>(a, k, gx, part); });
+        const auto go = [&]<int VV, int WARPS, int R>() {
+            with_flags(k.gs, !k.s, [&]<bool RES, bool Q8>() { norm_bwd_cols_kernel<T, VV, WARPS, R, RES, Q8><<<grid, WARPS * 32, 0, st>>>(a, k, gx, part); });
+        };
+        if (p.vec) with_cols(std::integral_constant<int, V>{}, p.form, go);
+        else with_cols(std::integral_constant<int, 1>{}, p.form, go);
     }
     const int rc = launched(1, "norm_bwd");
     if (rc || !gw) return rc;
-    if (p.held) norm_weight_sum_kernel<8><<<(unsigned)((a.C + 31) / 32), 256, 0, st>>>(a.C, p.blocks, part, gw);
+    if (p.form >= 0) norm_weight_sum_kernel<8><<<(unsigned)((a.C + 31) / 32), 256, 0, st>>>(a.C, p.blocks, part, gw);
     else norm_bwd_weight_any_kernel<T><<<(unsigned)a.C, 256, 0, st>>>(a, k, gw);
     return launched(1, "norm_bwd");
 }
@@ -266,7 +278,7 @@ size_t tconv_norm_workspace_bytes(const tconv_norm_desc_t* desc) {
     NormArgs a;
     if (check_norm(desc, &a)) return 0;
     const NormPlan p = plan_norm(a, desc->dtype);
-    return p.held ? (size_t)p.blocks * a.C * sizeof(float) : 0;
+    return p.form >= 0 ? (size_t)p.blocks * a.C * sizeof(float) : 0;
 }
 
 int tconv_norm_forward(const tconv_norm_desc_t* desc, const void* x, const void* residual, const float* weight, void* sum, void* y,
@@ -294,8 +306,7 @@ int tconv_norm_backward(const tconv_norm_desc_t* desc, const void* s, const void
     if (workspace_bytes < need || (need && !workspace)) return TCONV_ERR_WORKSPACE_TOO_SMALL;
     const NormIn k{s, (const int8_t*)s_codes, (const uint8_t*)s_scales, rstd, weight, grad_y, grad_sum};
     call_begins();
-    const auto run = desc->dtype == TCONV_F32 ? (s ? norm_bwd_t<float, false> : norm_bwd_t<float, true>)
-                                              : (s ? norm_bwd_t<__nv_bfloat16, false> : norm_bwd_t<__nv_bfloat16, true>);
+    const auto run = desc->dtype == TCONV_F32 ? norm_bwd_t<float> : norm_bwd_t<__nv_bfloat16>;
     return run(a, plan_norm(a, desc->dtype), k, grad_x, grad_weight, (float*)workspace, (cudaStream_t)stream);
 }
 
