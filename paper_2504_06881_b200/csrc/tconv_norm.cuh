@@ -280,6 +280,9 @@ __global__ void __launch_bounds__(WARPS * 32) norm_fwd_cols_kernel(const __grid_
 template <typename T, int V, int WARPS, int R, bool RES, bool Q8>
 __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_cols_kernel(
         const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k, T* __restrict__ gx, float* __restrict__ gw_part) {
+    // the stream's own gradient: read with the rest where registers allow, else in batches when it is added
+    constexpr bool kLate = V == 1 ? R > 16 : R > 4;
+    constexpr int kBatch = kLate ? R / 4 : R;
     __shared__ float part[WARPS][kQ8Block], total[kQ8Block];
     const Cols<V, WARPS> b;
     const uint32_t P = (uint32_t)a.P, tiles = (P + kQ8Block - 1) / kQ8Block, all = tiles * a.N, pitch = (uint32_t)q8_pitch(a.P);
@@ -295,7 +298,7 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
         const uint32_t at = b.c0 * P + p;
         const T *ps = (const T*)k.s + image, *py = (const T*)k.gy + image, *pg = (const T*)k.gs + image;
         Kept<T, V, Q8> s[R];
-        Some<T, V> dy[R], ds[RES ? R : 1];
+        Some<T, V> dy[R], ds[RES ? (kLate ? kBatch : R) : 1];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             s[j].none();
@@ -319,10 +322,13 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
                     rstd[i] = q.x; rstd[i + 1] = q.y; rstd[i + 2] = q.z; rstd[i + 3] = q.w;
                 }
         }
-        if constexpr (RES && V > 1)
+        if constexpr (RES && !kLate) {
 #pragma unroll
-            for (int j = 0; j < R; ++j)
+            for (int j = 0; j < R; ++j) {
+                ds[j] = none_of<T, V>();
                 if (j < live) ds[j] = load_some<T, V>(pg, at + j * step);
+            }
+        }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const float wc = j < have ? __ldg(k.w + b.c0 + j * b.kStep) : 0.0f;
@@ -339,22 +345,31 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
         b.sum(m, part, total, [&](float t, int) { return t / (float)a.C; });
         T* po = gx + image;
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            if (j >= live) continue;
-            const float wc = __ldg(k.w + b.c0 + j * b.kStep);
-            float v[V], d[V];
-            s[j].values(v);
-            spread<T, V>(dy[j], d);
+        for (int j0 = 0; j0 < R; j0 += kBatch) {
+            if constexpr (RES && kLate) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) d[i] = rstd[i] * (wc * d[i] - v[i] * rstd[i] * m[i]);
-            if constexpr (RES) {
-                float e[V];
-                if constexpr (V > 1) spread<T, V>(ds[j], e);
-                else spread<T, V>(load_some<T, V>(pg, at + j * step), e);
-#pragma unroll
-                for (int i = 0; i < V; ++i) d[i] += e[i];
+                for (int j = 0; j < kBatch; ++j) {
+                    ds[j] = none_of<T, V>();
+                    if (j0 + j < live) ds[j] = load_some<T, V>(pg, at + (j0 + j) * step);
+                }
             }
-            store_some<T, V>(po, at + j * step, gather<T, V>(d));
+#pragma unroll
+            for (int jj = 0; jj < kBatch; ++jj) {
+                const int j = j0 + jj;
+                const float wc = j < have ? __ldg(k.w + b.c0 + j * b.kStep) : 0.0f;
+                float v[V], d[V];
+                s[j].values(v);
+                spread<T, V>(dy[j], d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) d[i] = rstd[i] * (wc * d[i] - v[i] * rstd[i] * m[i]);
+                if constexpr (RES) {
+                    float e[V];
+                    spread<T, V>(ds[kLate ? jj : j], e);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) d[i] += e[i];
+                }
+                if (j < live) store_some<T, V>(po, at + j * step, gather<T, V>(d));
+            }
         }
     }
     if (!gw_part) return;
