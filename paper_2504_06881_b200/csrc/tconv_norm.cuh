@@ -106,31 +106,18 @@ template <typename T, int V> __device__ __forceinline__ Some<T, V> gather(const 
 // Stores V values of an 8-bit form: codes to `to`, and at a block's first value the scale byte to `scale`; the 32 / V lanes of a block
 // are neighbours, and every lane of the warp calls.  ok: the values are there to be stored.
 template <int V> __device__ __forceinline__ void q8_put_some(const float (&v)[V], bool ok, int8_t* to, bool head, uint8_t* scale) {
-    uint32_t top = magnitude_bits(v[0]);
-#pragma unroll
-    for (int i = 1; i < V; ++i) top = max(top, magnitude_bits(v[i]));
+    uint32_t top = __float_as_uint(top_of(v));
     if constexpr (V == 1) top = __reduce_max_sync(~0u, top);
     else
 #pragma unroll
         for (int d = 1; d < kQ8Block / V; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
     const uint32_t byte = q8_scale_byte(top);
     if (!ok) return;
-    uint32_t b[V];
-    const float inv = q8_inverse(byte);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {    // (1.5 * 2^23 has unit 1: the code is the sum's low byte)
-        const float t = __fadd_rn(__fmul_rn(v[i], inv), 12582912.0f);
-        b[i] = byte == 255u ? 0u : __float_as_uint(t);
-    }
-    if constexpr (V == 1) *to = (int8_t)b[0];
-    else {
-        uint32_t w[V / 4];
-#pragma unroll
-        for (int i = 0; i < V / 4; ++i)
-            w[i] = __byte_perm(__byte_perm(b[4 * i], b[4 * i + 1], 0x0040), __byte_perm(b[4 * i + 2], b[4 * i + 3], 0x0040), 0x5410);
-        if constexpr (V == 4) *reinterpret_cast<uint32_t*>(to) = w[0];
-        else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-    }
+    float r[V];
+    q8_round(v, byte, r);
+    if constexpr (V == 1) *to = (int8_t)__float_as_uint(r[0]);
+    else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(to) = four_codes(r);
+    else *reinterpret_cast<uint2*>(to) = make_uint2(four_codes(r), four_codes(r + 4));
     if (head) *scale = (uint8_t)byte;
 }
 
@@ -159,8 +146,10 @@ template <typename T, int V> struct Kept<T, V, true> {
     }
     __device__ __forceinline__ void values(float (&v)[V]) const {
         const float unit = q8_unit(byte);
+        if constexpr (V == 1) v[0] = (float)(int8_t)w[0] * unit;
+        else
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i & 3))) * unit;
+            for (int i = 0; i < V; i += 4) decode_four(w[i / 4], unit, v + i);
     }
 };
 

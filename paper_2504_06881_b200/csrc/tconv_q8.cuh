@@ -33,37 +33,58 @@ __device__ __forceinline__ int q8_code(float v, uint32_t byte) {
     return byte == 255u ? 0 : __float2int_rn(v * q8_inverse(byte));
 }
 
+// Largest magnitude of N values; NaN if one of them is.
+template <int N> __device__ __forceinline__ float top_of(const float (&v)[N]) {
+    float m = fabsf(v[0]);
+#pragma unroll
+    for (int i = 1; i + 1 < N; i += 2) asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(v[i]), "f"(v[i + 1]));
+    if constexpr (N % 2 == 0) asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(v[N - 1]));
+    return fabsf(m);
+}
 // Scale byte of the block that v is part of: a thread has eight values of it, and its four threads are neighbours (G = 1: a row
 // of at most eight values, one thread's).
 template <int G> __device__ __forceinline__ uint32_t block_scale(const float (&v)[8]) {
-    uint32_t top = magnitude_bits(v[0]);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = max(top, magnitude_bits(v[i]));
+    uint32_t top = __float_as_uint(top_of(v));
     if constexpr (G > 1) {
         top = max(top, __shfl_xor_sync(~0u, top, 1));
         top = max(top, __shfl_xor_sync(~0u, top, 2));
     }
     return q8_scale_byte(top);
 }
-// v becomes the values its codes stand for.  Rounded by adding 1.5 * 2^23, whose unit is 1: the code is the sum's low byte.
-__device__ __forceinline__ uint2 encode_eight(float (&v)[8], uint32_t byte) {
-    const float inv = q8_inverse(byte), unit = q8_unit(byte), magic = 12582912.0f;
-    uint32_t b[8];
+// v * 2^-e + 1.5 * 2^23: the sum's unit is 1, so that its low byte is the code, rounded half to even.
+constexpr float kQ8Magic = 12582912.0f;
+template <int N> __device__ __forceinline__ void q8_round(const float (&v)[N], uint32_t byte, float (&r)[N]) {
+    const float inv = q8_inverse(byte);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float r = byte == 255u ? magic : __fadd_rn(__fmul_rn(v[i], inv), magic);
-        b[i] = __float_as_uint(r);
-        v[i] = __fsub_rn(r, magic) * unit;
-    }
-    const auto four = [&](int i) {
-        return __byte_perm(__byte_perm(b[i], b[i + 1], 0x0040), __byte_perm(b[i + 2], b[i + 3], 0x0040), 0x5410);
-    };
-    return make_uint2(four(0), four(4));
+    for (int i = 0; i < N; ++i) r[i] = fmaf(v[i], inv, kQ8Magic);
+    if (byte == 255u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[i] = kQ8Magic;
+}
+__device__ __forceinline__ uint32_t four_codes(const float* r) {
+    return __byte_perm(__byte_perm(__float_as_uint(r[0]), __float_as_uint(r[1]), 0x0040),
+                       __byte_perm(__float_as_uint(r[2]), __float_as_uint(r[3]), 0x0040), 0x5410);
+}
+// Codes of v, which becomes the values that they stand for.
+__device__ __forceinline__ uint2 encode_eight(float (&v)[8], uint32_t byte) {
+    float r[8];
+    q8_round(v, byte, r);
+    const float unit = q8_unit(byte);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(__fadd_rn(r[i], -kQ8Magic), unit);
+    return make_uint2(four_codes(r), four_codes(r + 4));
+}
+// A word's four values: code + 128 as the low byte of a float of unit 1.
+__device__ __forceinline__ void decode_four(uint32_t w, float unit, float* v) {
+    w ^= 0x80808080u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = __fmul_rn(__fadd_rn(__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + i)), -8388736.0f), unit);
 }
 __device__ __forceinline__ void decode_eight(uint2 c, uint32_t byte, float (&v)[8]) {
     const float unit = q8_unit(byte);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3))) * unit;
+    decode_four(c.x, unit, v);
+    decode_four(c.y, unit, v + 4);
 }
 
 // A thread has 8 values of a row; four neighbours are a block (a row's last block may have idle ones).  I: the type that counts

@@ -63,17 +63,17 @@ bool rows_aligned(const void* p, int64_t batch, int64_t row, int64_t L, int64_t 
 
 enum { kFwd, kBwd };
 
-template <int DIR, typename T, bool Q8, int ACC, int G, bool MULTI, bool JOIN, typename IO>
+template <int DIR, typename T, bool Q8, int ACC, int G, int MODE, typename IO>
 void scan_launch(const ScanArgs& a, const ScanPlan& p, const IO& io, cudaStream_t st) {
     const auto kern = [] {
-        if constexpr (DIR == kFwd) return scan_fwd_kernel<T, Q8, ACC, G, MULTI, JOIN>;
-        else return scan_bwd_kernel<T, Q8, ACC, G, MULTI, JOIN>;
+        if constexpr (DIR == kFwd) return scan_fwd_kernel<T, Q8, ACC, G, MODE>;
+        else return scan_bwd_kernel<T, Q8, ACC, G, MODE>;
     }();
-    if constexpr (MULTI) {
-        kern<<<dim3((unsigned)a.rows, (unsigned)p.parts), p.warps * 32, 0, st>>>(a, io);
+    if constexpr (MODE == kBlock) {
+        kern<<<(unsigned)a.rows, p.warps * 32, 0, st>>>(a, io);
     } else {
         const int64_t per = 4 * (32 / G);
-        kern<<<(unsigned)((a.rows + per - 1) / per), 128, 0, st>>>(a, io);
+        kern<<<(unsigned)((a.rows * p.parts + per - 1) / per), 128, 0, st>>>(a, io);
     }
 }
 
@@ -81,17 +81,17 @@ template <int DIR, typename T, bool Q8, bool VEC, typename IO>
 int scan_run(const ScanArgs& a, const ScanPlan& p, const IO& io, cudaStream_t st) {
     constexpr int kLong = VEC ? kVector : kStaged, kShort = VEC ? kVector : kStraight;
     const char* name = DIR == kFwd ? "scan_fwd" : "scan_bwd";
-    if (p.g == 1) scan_launch<DIR, T, Q8, kShort, 1, false, false>(a, p, io, st);
-    else if (p.g == 4) scan_launch<DIR, T, Q8, kShort, 4, false, false>(a, p, io, st);
-    else if (p.g == 16) scan_launch<DIR, T, Q8, kShort, 16, false, false>(a, p, io, st);
-    else if (p.warps == 1) scan_launch<DIR, T, Q8, kLong, 32, false, false>(a, p, io, st);
+    if (p.g == 1) scan_launch<DIR, T, Q8, kShort, 1, kWarp>(a, p, io, st);
+    else if (p.g == 4) scan_launch<DIR, T, Q8, kShort, 4, kWarp>(a, p, io, st);
+    else if (p.g == 16) scan_launch<DIR, T, Q8, kShort, 16, kWarp>(a, p, io, st);
+    else if (p.warps > 1) scan_launch<DIR, T, Q8, kLong, 32, kBlock>(a, p, io, st);
     else {
         if (p.parts > 1) {
-            scan_launch<DIR, T, Q8, kLong, 32, true, true>(a, p, io, st);
+            scan_launch<DIR, T, Q8, kLong, 32, kJoin>(a, p, io, st);
             const int rc = launched(1, name);
             if (rc) return rc;
         }
-        scan_launch<DIR, T, Q8, kLong, 32, true, false>(a, p, io, st);
+        scan_launch<DIR, T, Q8, kLong, 32, kWarp>(a, p, io, st);
     }
     return launched(1, name);
 }
