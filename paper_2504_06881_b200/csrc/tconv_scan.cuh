@@ -17,9 +17,10 @@ constexpr int kScanChunk = 256;      // positions per warp and step; between two
 constexpr int kScanWarps = 8;        // most warps of a block on one row
 constexpr int kScanParts = 256;      // most parts of a row
 
-// How a thread's positions are read and written: whole vectors where every row starts on 16 bytes; else lane by lane
-// through shared memory (8 positions a thread, straight, would touch every sector eight times), straight for short rows.
-enum ScanAccess { kVector, kStaged, kStraight };
+// How a thread's positions are read and written.  kRing: chunk by chunk through shared memory, two chunks ahead, in whole
+// 16-byte vectors whatever the rows' alignment (see Ring).  Rows of at most 128 positions: whole vectors where every row starts
+// on 16 bytes (kVector), value by value elsewhere (kStraight).
+enum ScanAccess { kVector, kStraight, kRing };
 
 struct ScanArgs {
     int64_t rows;
@@ -102,84 +103,147 @@ __device__ __forceinline__ void pack(const float (&v)[8], Words<__nv_bfloat16>& 
     r.w[0] = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The values of positions [at, at + 8) of a row below `end` (what a vector holds behind it is not masked).  fetch() starts the loads, take() hands them out.
-// Staged: a warp's 256 positions from `chunk_at`, through its `stage` of shared memory.
-template <typename T, int ACC> struct Eight {
-    Words<T> r;
-    T s[ACC == kVector ? 1 : kScanVec];
-
-    __device__ __forceinline__ void fetch(const T* __restrict__ row, uint32_t at, uint32_t end) {
-        if constexpr (ACC == kVector) {
+// The values of positions [at, at + 8) of a row below `end` (what a vector holds behind it is not masked).
+template <typename T, int ACC> __device__ __forceinline__ void get_eight(const T* __restrict__ row, uint32_t at, uint32_t end, float (&v)[8]) {
+    if constexpr (ACC == kVector) {
+        Words<T> r;
 #pragma unroll
-            for (int j = 0; j < Words<T>::n; ++j) {
-                r.w[j] = make_uint4(0, 0, 0, 0);
-                if (at + j * Words<T>::per < end) r.w[j] = __ldg(reinterpret_cast<const uint4*>(row + at) + j);
-            }
-        } else {
-            constexpr int kStride = ACC == kStaged ? 32 : 1;
-            const uint32_t lane = threadIdx.x & 31, first = ACC == kStaged ? at - kScanVec * lane + lane : at;
-            const T* p = row + first;
-            if (ACC == kStaged && first - lane + kScanChunk <= end) {       // (the same for the whole warp)
-#pragma unroll
-                for (int i = 0; i < kScanVec; ++i) s[i] = __ldg(p + i * kStride);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kScanVec; ++i) {
-                    s[i] = zero_of<T>();
-                    if (first + i * kStride < end) s[i] = __ldg(p + i * kStride);
-                }
-            }
+        for (int j = 0; j < Words<T>::n; ++j) {
+            r.w[j] = make_uint4(0, 0, 0, 0);
+            if (at + j * Words<T>::per < end) r.w[j] = __ldg(reinterpret_cast<const uint4*>(row + at) + j);
         }
-    }
-    __device__ __forceinline__ void take(float (&v)[8], T* stage) {
-        if constexpr (ACC == kStraight) {
+        unpack(r, v);
+    } else {
+        T s[8];
 #pragma unroll
-            for (int i = 0; i < kScanVec; ++i) v[i] = to_f32(s[i]);
-        } else {
-            if constexpr (ACC == kStaged) {
-                const uint32_t lane = threadIdx.x & 31;
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < kScanVec; ++i) stage[32 * i + lane] = s[i];
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < Words<T>::n; ++j) r.w[j] = reinterpret_cast<const uint4*>(stage + kScanVec * lane)[j];
-            }
-            unpack(r, v);
+        for (int i = 0; i < kScanVec; ++i) {
+            s[i] = zero_of<T>();
+            if (at + i < end) s[i] = __ldg(row + at + i);
         }
+#pragma unroll
+        for (int i = 0; i < kScanVec; ++i) v[i] = to_f32(s[i]);
     }
-};
-
-// Writes the values of positions [at, at + 8) below `end`.
-template <typename T, int ACC>
-__device__ __forceinline__ void put_eight(T* __restrict__ row, uint32_t at, uint32_t end, const float (&v)[8], T* stage) {
-    if constexpr (ACC == kStraight) {
+}
+template <typename T, int ACC> __device__ __forceinline__ void put_eight(T* __restrict__ row, uint32_t at, uint32_t end, const float (&v)[8]) {
+    if constexpr (ACC == kVector) {
+        Words<T> r;
+        pack(v, r);
+#pragma unroll
+        for (int j = 0; j < Words<T>::n; ++j)
+            if (at + j * Words<T>::per < end) reinterpret_cast<uint4*>(row + at)[j] = r.w[j];
+    } else {
 #pragma unroll
         for (int i = 0; i < kScanVec; ++i)
             if (at + i < end) row[at + i] = from_f32<T>(v[i]);
-    } else {
-        Words<T> r;
-        pack(v, r);
-        if constexpr (ACC == kVector) {
+    }
+}
+
+// Four words from word S of w on, shifted down by `bits` (0 or 16) across them.
+template <int S, int N> __device__ __forceinline__ uint4 four_words(const uint32_t (&w)[N], uint32_t bits) {
+    return make_uint4(__funnelshift_r(w[S], w[S + 1], bits), __funnelshift_r(w[S + 1], w[S + 2], bits),
+                      __funnelshift_r(w[S + 2], w[S + 3], bits), S + 4 < N ? __funnelshift_r(w[S + 3], w[S + 4 < N ? S + 4 : 0], bits) : w[S + 3]);
+}
+// 16 bytes that start `shift` bytes (the same in the whole warp) into the 32 of lo and hi.
+__device__ __forceinline__ uint4 across(uint4 lo, uint4 hi, uint32_t shift) {
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, bits = (shift & 2) * 8;
+    switch (shift >> 2) {
+        case 0: return four_words<0>(w, bits);
+        case 1: return four_words<1>(w, bits);
+        case 2: return four_words<2>(w, bits);
+        default: return four_words<3>(w, bits);
+    }
+}
+
+// A warp's chunks of one row on their way through shared memory.  The copies are those of the aligned 16-byte vectors that hold
+// the chunk: they start up to 15 bytes before it and end as far behind it (always within 16 bytes that hold some value of the
+// row), and the values are taken out of neighbouring vectors by a shift that the whole row shares.
+template <typename T> struct Ring {
+    static constexpr int kBytes = kScanChunk * (int)sizeof(T), kVectors = kBytes / 16, kSlot = kBytes + 16, kSlots = 2;
+    const char* from;                // the row's start, rounded down
+    uint32_t shift, live;            // its distance from there in bytes; the positions to be read
+    char* slots;
+    __device__ __forceinline__ Ring(const T* row, uint32_t live, char* to)
+        : from(reinterpret_cast<const char*>(row) - (reinterpret_cast<uintptr_t>(row) & 15)),
+          shift((uint32_t)reinterpret_cast<uintptr_t>(row) & 15), live(live), slots(to) {}
+    __device__ __forceinline__ static void copy(char* to, const char* src, uint32_t bytes) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(src), "r"(bytes) : "memory");
+    }
+    // Starts the copies of a chunk; what lies behind the row's length becomes zero.
+    __device__ __forceinline__ void fetch(uint32_t chunk, int slot) {
+        const uint32_t lane = threadIdx.x & 31;
+        const char* src = from + (int64_t)chunk * kBytes;
+        char* to = slots + slot * kSlot;
+        if ((chunk + 1) * kScanChunk <= live) {
 #pragma unroll
-            for (int j = 0; j < Words<T>::n; ++j)
-                if (at + j * Words<T>::per < end) reinterpret_cast<uint4*>(row + at)[j] = r.w[j];
+            for (int j = 0; j < kVectors / 32; ++j) copy(to + 16 * (32 * j + lane), src + 16 * (32 * j + lane), 16);
+            if (shift && lane == 0) copy(to + kBytes, src + kBytes, shift);
         } else {
-            const uint32_t lane = threadIdx.x & 31, first = at - kScanVec * lane + lane;
-            __syncwarp();
+            const uint32_t first = chunk * kScanChunk, left = first < live ? shift + (live - first) * (uint32_t)sizeof(T) : 0;
 #pragma unroll
-            for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(stage + kScanVec * lane)[j] = r.w[j];
-            __syncwarp();
-            T* p = row + first;
-            if (first - lane + kScanChunk <= end) {
-#pragma unroll
-                for (int i = 0; i < kScanVec; ++i) p[32 * i] = stage[32 * i + lane];
-            } else {
-#pragma unroll
-                for (int i = 0; i < kScanVec; ++i)
-                    if (first + 32 * i < end) p[32 * i] = stage[32 * i + lane];
+            for (int j = 0; j < kVectors / 32 + 1; ++j) {
+                const uint32_t b = 16 * (32 * j + lane);
+                if (j == kVectors / 32 && lane) break;
+                const uint32_t n = b < left ? min(left - b, 16u) : 0;
+                copy(to + b, n ? src + b : from, n);
             }
         }
+    }
+    // This lane's eight values of a chunk that has arrived.
+    __device__ __forceinline__ void take(int slot, float (&v)[8]) const {
+        const uint4* p = reinterpret_cast<const uint4*>(slots + slot * kSlot) + (threadIdx.x & 31) * Words<T>::n;
+        Words<T> r;
+#pragma unroll
+        for (int j = 0; j < Words<T>::n; ++j) r.w[j] = p[j];
+        if (shift) {
+            const uint4 next = p[Words<T>::n];
+#pragma unroll
+            for (int j = 0; j < Words<T>::n; ++j) r.w[j] = across(r.w[j], j + 1 < Words<T>::n ? r.w[j + 1] : next, shift);
+        }
+        unpack(r, v);
+    }
+};
+__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void ring_wait() {      // all but the newest group are there
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncwarp();
+}
+
+// Writes a warp's chunk below `end`, in whole vectors: those of an unaligned row are put together across lanes in `stage`, and what
+// is left of the first and the last (16 bytes in all) goes value by value.
+template <typename T> __device__ __forceinline__ void put_chunk(T* __restrict__ row, uint32_t chunk, uint32_t end, const float (&v)[8], char* stage) {
+    constexpr int kPer = Words<T>::per;
+    const uint32_t lane = threadIdx.x & 31, first = chunk * kScanChunk;
+    if (first >= end) return;
+    T* to = row + first;
+    const uint32_t shift = (uint32_t)reinterpret_cast<uintptr_t>(to) & 15;
+    const bool whole = first + kScanChunk <= end;
+    Words<T> r;
+    pack(v, r);
+    if (whole && !shift) {
+#pragma unroll
+        for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(to)[Words<T>::n * lane + j] = r.w[j];
+        return;
+    }
+    uint4* s = reinterpret_cast<uint4*>(stage);
+    const T* values = reinterpret_cast<const T*>(stage);
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < Words<T>::n; ++j) s[Words<T>::n * lane + j] = r.w[j];
+    __syncwarp();
+    if (whole) {
+        uint4* aligned = reinterpret_cast<uint4*>(reinterpret_cast<char*>(to) - shift);
+#pragma unroll
+        for (int j = 0; j < Words<T>::n; ++j) {
+            const uint32_t q = 32 * j + lane;
+            const uint4 lo = s[q ? q - 1 : 0], w = across(lo, s[q], 16 - shift);
+            if (q) aligned[q] = w;
+        }
+        const uint32_t e = lane + shift / (uint32_t)sizeof(T) < kPer ? lane : kScanChunk - kPer + lane;
+        if (lane < kPer) to[e] = values[e];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kScanVec; ++i)
+            if (first + 32 * i + lane < end) to[32 * i + lane] = values[32 * i + lane];
     }
 }
 
@@ -258,15 +322,18 @@ template <int G, int MODE> struct Place {
     }
 };
 
+// Shared memory of a warp: rings, and a chunk to be written.
+template <typename T> __host__ __device__ constexpr int scan_space(int rings, bool writes) {
+    return rings * Ring<T>::kSlots * Ring<T>::kSlot + (writes ? Ring<T>::kBytes : 0);
+}
+
 // Forward.
 template <typename T, bool Q8, int ACC, int G, int MODE>
 __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_fwd_kernel(const __grid_constant__ ScanArgs a,
                                                                                           const __grid_constant__ ScanFwd io) {
-    constexpr int kStages = ACC == kStaged ? (MODE == kBlock ? kScanWarps : 4) : 1;
-    __shared__ __align__(16) T stages[kStages][ACC == kStaged ? 2 * kScanChunk : 16];
+    extern __shared__ __align__(16) char ring_space[];        // a warp's: slots of x, of gate, and a chunk to be written
     __shared__ Map shared[MODE == kBlock ? 2 : 1][kScanWarps], shared_q[MODE == kBlock && Q8 ? 2 : 1][kScanWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = MODE == kBlock ? blockDim.x >> 5 : 1, sub = lane % G;
-    T *stage = stages[ACC == kStaged ? warp : 0], *stage_g = stage + (ACC == kStaged ? kScanChunk : 0);
     const Place<G, MODE> at_row(a);
     if (!at_row.any) return;
     const int64_t row = at_row.row, n = row / a.C, c = row - n * a.C;
@@ -291,19 +358,31 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
                 if constexpr (Q8) hq = apply(warp_join({m.z, m.w}), hq);
             }
     }
-    Eight<T, ACC> rx, rg;
-    uint32_t at = (k_begin + (MODE == kBlock ? warp : 0)) * kScanChunk + sub * kScanVec;
-    rx.fetch(px, at, end);
-    rg.fetch(pg, at, end);
+    constexpr bool kChunks = ACC == kRing;
+    using R = Ring<T>;
+    char* space = ring_space + (kChunks ? warp * scan_space<T>(2, MODE != kJoin) : 0);
+    R rx(px, end, space), rg(pg, end, space + R::kSlots * R::kSlot);
+    char* stage = space + 2 * R::kSlots * R::kSlot;
+    const auto fetch = [&](uint32_t k, int slot) {
+        const uint32_t chunk = k + (MODE == kBlock ? warp : 0);
+        if (k < k_end && chunk * kScanChunk < end) {
+            rx.fetch(chunk, slot);
+            rg.fetch(chunk, slot);
+        }
+        ring_commit();
+    };
+    if constexpr (kChunks) {
+        fetch(k_begin, 0);
+        fetch(k_begin + warps, 1);
+    }
     int turn = 0;
     for (uint32_t k = k_begin; k < k_end; k += warps, turn ^= 1) {
-        const uint32_t here = at, chunk = k + (MODE == kBlock ? warp : 0);
-        at += warps * kScanChunk;
-        if (G == 32 && MODE != kBlock && k * kScanChunk >= end) {          // behind the row's length, with all that follows
+        const uint32_t chunk = k + (MODE == kBlock ? warp : 0), here = chunk * kScanChunk + sub * kScanVec;
+        if (kChunks && MODE != kBlock && chunk * kScanChunk >= end) {      // behind the row's length, with all that follows
             if constexpr (MODE == kJoin) break;
             else {
                 const float zero[8] = {};
-                put_eight<T, ACC>(py, here, L, zero, stage);
+                put_chunk(py, chunk, L, zero, stage);
                 if (io.states && sub == 0) io.states[row * a.chunks + chunk] = Q8 ? hq : h;
                 if constexpr (Q8)
                     if (here < (uint32_t)pitch) {
@@ -314,14 +393,18 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
             }
         }
         float x[8], g[8], f[8], b[8];
-        rx.take(x, stage);
-        rg.take(g, stage_g);
-        if (G == 32 && k + warps < k_end) {                   // the next chunk is on its way while this one is worked on
-            rx.fetch(px, at, end);
-            rg.fetch(pg, at, end);
+        if constexpr (kChunks) {
+            ring_wait();
+            rx.take(turn, x);
+            rg.take(turn, g);
+            __syncwarp();
+            fetch(k + 2 * warps, turn);                       // two chunks ahead, into the slot just read
+        } else {
+            get_eight<T, ACC>(px, here, end, x);
+            get_eight<T, ACC>(pg, here, end, g);
         }
         const int live = end <= here ? 0 : (int)min(end - here, (uint32_t)kScanVec);
-        if constexpr (Q8 && ACC == kVector) {                 // what a vector holds behind the row's length is no part of a block
+        if constexpr (Q8) {                                   // what lies behind the row's length is no part of a block
             if (live < 8)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -410,9 +493,11 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
                 for (int i = 0; i < 8; ++i)
                     if (i >= live) y[i] = 0.0f;
             }
-            put_eight<T, ACC>(py, here, L, y, stage);
+            if constexpr (kChunks) put_chunk(py, chunk, L, y, stage);
+            else put_eight<T, ACC>(py, here, L, y);
         }
     }
+    if constexpr (kChunks) asm volatile("cp.async.wait_all;" ::: "memory");
     if constexpr (MODE == kJoin) {
         if (lane == 0) a.joined[row * a.parts + at_row.part] = make_float4(total.P, total.B, total_q.P, total_q.B);
     } else {
@@ -425,12 +510,9 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
 template <typename T, bool Q8, int ACC, int G, int MODE>
 __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_bwd_kernel(const __grid_constant__ ScanArgs a,
                                                                                           const __grid_constant__ ScanBwd io) {
-    constexpr int kStages = ACC == kStaged ? (MODE == kBlock ? kScanWarps : 4) : 1;
-    __shared__ __align__(16) T stages[kStages][ACC == kStaged ? 3 * kScanChunk : 16];
+    extern __shared__ __align__(16) char ring_space[];        // a warp's: slots of grad_y and, not kept in 8 bits, gate and x; a chunk
     __shared__ Map shared[MODE == kBlock ? 2 : 1][kScanWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = MODE == kBlock ? blockDim.x >> 5 : 1, sub = lane % G;
-    constexpr int kOff = ACC == kStaged ? kScanChunk : 0;
-    T* stage = stages[ACC == kStaged ? warp : 0];
     const Place<G, MODE> at_row(a);
     if (!at_row.any) return;
     const int64_t row = at_row.row, n = row / a.C, c = row - n * a.C;
@@ -455,13 +537,30 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
                 E = apply(warp_join({m.x, m.y}), E);
             }
     }
-    Eight<T, ACC> rx, rg, ry;
+    constexpr bool kChunks = ACC == kRing;
+    constexpr int kRings = Q8 ? 1 : MODE == kJoin ? 2 : 3;
+    using R = Ring<T>;
+    char* space = ring_space + (kChunks ? warp * scan_space<T>(kRings, MODE != kJoin) : 0);
+    R ry(py, end, space), rg(pg, end, space + R::kSlots * R::kSlot), rx(px, end, space + 2 * R::kSlots * R::kSlot);
+    char* stage = space + kRings * R::kSlots * R::kSlot;
+    const uint32_t steps = (k_end - k_begin + warps - 1) / warps;
+    // step j works on the chunks from k_begin + j * warps on; from the last step down
+    const auto chunk_of = [&](uint32_t j) { return k_begin + j * warps + (MODE == kBlock ? warp : 0); };
+    const auto fetch = [&](uint32_t j, int slot) {            // (j wraps below zero: beyond steps)
+        if (j < steps && chunk_of(j) * kScanChunk < end) {
+            ry.fetch(chunk_of(j), slot);
+            if constexpr (!Q8) {
+                rg.fetch(chunk_of(j), slot);
+                if constexpr (MODE != kJoin) rx.fetch(chunk_of(j), slot);
+            }
+        }
+        ring_commit();
+    };
     uint2 cx, cg;
     uint32_t bx, bg;
     float state;
-    const auto fetch = [&](uint32_t k) {
-        const uint32_t chunk = k + (MODE == kBlock ? warp : 0), at = chunk * kScanChunk + sub * kScanVec;
-        ry.fetch(py, at, end);
+    const auto fetch_kept = [&](uint32_t j) {
+        const uint32_t at = chunk_of(j) * kScanChunk + sub * kScanVec;
         if constexpr (Q8) {
             cx = cg = make_uint2(0, 0);
             bx = bg = 1;
@@ -473,38 +572,50 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
                     bx = __ldg(xs + at / kQ8Block);
                 }
             }
-        } else {
-            rg.fetch(pg, at, end);
-            if (MODE != kJoin) rx.fetch(px, at, end);
         }
-        if (MODE != kJoin) state = chunk < a.chunks ? __ldg(io.states + row * a.chunks + chunk) : 0.0f;
+        if (MODE != kJoin) state = chunk_of(j) < a.chunks ? __ldg(io.states + row * a.chunks + chunk_of(j)) : 0.0f;
     };
-    uint32_t steps = (k_end - k_begin + warps - 1) / warps;
-    if (G == 32 && MODE != kBlock) {                          // chunks behind the row's length
-        for (; steps && (k_begin + steps - 1) * kScanChunk >= end; --steps) {
+    uint32_t j = steps - 1;
+    if constexpr (kChunks && MODE != kBlock) {                // chunks behind the row's length
+        for (; j < steps && chunk_of(j) * kScanChunk >= end; --j) {
             if constexpr (MODE != kJoin) {
-                const uint32_t here = (k_begin + steps - 1) * kScanChunk + sub * kScanVec;
                 const float zero[8] = {};
-                put_eight<T, ACC>(ox, here, L, zero, stage);
-                put_eight<T, ACC>(og, here, L, zero, stage + kOff);
+                put_chunk(ox, chunk_of(j), L, zero, stage);
+                put_chunk(og, chunk_of(j), L, zero, stage);
             }
         }
     }
-    if (steps) fetch(k_begin + (steps - 1) * warps);
+    if (j < steps) fetch_kept(j);
+    if constexpr (kChunks) {
+        fetch(j, 0);
+        fetch(j - 1, 1);
+    }
     int turn = 0;
-    for (; steps; --steps, turn ^= 1) {
-        const uint32_t here = (k_begin + (steps - 1) * warps + (MODE == kBlock ? warp : 0)) * kScanChunk + sub * kScanVec;
+    for (; j < steps; --j, turn ^= 1) {
+        const uint32_t chunk = chunk_of(j), here = chunk * kScanChunk + sub * kScanVec;
         float x[8], g[8], d[8], f[8], u[8];
-        ry.take(d, stage);
+        if constexpr (kChunks) {
+            ring_wait();
+            ry.take(turn, d);
+            if constexpr (!Q8) {
+                rg.take(turn, g);
+                if constexpr (MODE != kJoin) rx.take(turn, x);
+            }
+            __syncwarp();
+            fetch(j - 2, turn);                               // two steps ahead, into the slot just read
+        } else {
+            get_eight<T, ACC>(py, here, end, d);
+            if constexpr (!Q8) {
+                get_eight<T, ACC>(pg, here, end, g);
+                get_eight<T, ACC>(px, here, end, x);
+            }
+        }
         if constexpr (Q8) {
             decode_eight(cg, bg, g);
             if (MODE != kJoin) decode_eight(cx, bx, x);
-        } else {
-            rg.take(g, stage + kOff);
-            if (MODE != kJoin) rx.take(x, stage + 2 * kOff);
         }
         const float first = state;
-        if (G == 32 && steps > 1) fetch(k_begin + (steps - 2) * warps);
+        if (kChunks && j > 0) fetch_kept(j - 1);
         const int live = end <= here ? 0 : (int)min(end - here, (uint32_t)kScanVec);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -558,10 +669,16 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
                 for (int i = 0; i < 8; ++i)
                     if (i >= live) x[i] = g[i] = 0.0f;
             }
-            put_eight<T, ACC>(ox, here, L, x, stage);
-            put_eight<T, ACC>(og, here, L, g, stage + kOff);
+            if constexpr (kChunks) {
+                put_chunk(ox, chunk, L, x, stage);
+                put_chunk(og, chunk, L, g, stage);
+            } else {
+                put_eight<T, ACC>(ox, here, L, x);
+                put_eight<T, ACC>(og, here, L, g);
+            }
         }
     }
+    if constexpr (kChunks) asm volatile("cp.async.wait_all;" ::: "memory");
     if constexpr (MODE == kJoin) {
         if (lane == 0) a.joined[row * a.parts + at_row.part] = make_float4(total.P, total.B, 1.0f, 0.0f);
     } else {

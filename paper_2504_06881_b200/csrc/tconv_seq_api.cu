@@ -69,29 +69,33 @@ void scan_launch(const ScanArgs& a, const ScanPlan& p, const IO& io, cudaStream_
         if constexpr (DIR == kFwd) return scan_fwd_kernel<T, Q8, ACC, G, MODE>;
         else return scan_bwd_kernel<T, Q8, ACC, G, MODE>;
     }();
-    if constexpr (MODE == kBlock) {
-        kern<<<(unsigned)a.rows, p.warps * 32, 0, st>>>(a, io);
-    } else {
-        const int64_t per = 4 * (32 / G);
-        kern<<<(unsigned)((a.rows * p.parts + per - 1) / per), 128, 0, st>>>(a, io);
-    }
+    constexpr int kRings = DIR == kFwd ? 2 : Q8 ? 1 : MODE == kJoin ? 2 : 3;
+    const int warps = MODE == kBlock ? p.warps : 4, smem = ACC == kRing ? warps * scan_space<T>(kRings, MODE != kJoin) : 0;
+    const int64_t warps_needed = G == 32 ? a.rows * p.parts : (a.rows + 32 / G - 1) / (32 / G);
+    if (smem > 48 * 1024 && allow_smem(kern, smem) != cudaSuccess) return;       // (its error is what launched() finds)
+    kern<<<(unsigned)(MODE == kBlock ? a.rows : (warps_needed + 3) / 4), warps * 32, smem, st>>>(a, io);
 }
 
-template <int DIR, typename T, bool Q8, bool VEC, typename IO>
-int scan_run(const ScanArgs& a, const ScanPlan& p, const IO& io, cudaStream_t st) {
-    constexpr int kLong = VEC ? kVector : kStaged, kShort = VEC ? kVector : kStraight;
+template <int DIR, typename T, bool Q8, typename IO>
+int scan_run(const ScanArgs& a, const ScanPlan& p, const IO& io, bool vec, cudaStream_t st) {
     const char* name = DIR == kFwd ? "scan_fwd" : "scan_bwd";
-    if (p.g == 1) scan_launch<DIR, T, Q8, kShort, 1, kWarp>(a, p, io, st);
-    else if (p.g == 4) scan_launch<DIR, T, Q8, kShort, 4, kWarp>(a, p, io, st);
-    else if (p.g == 16) scan_launch<DIR, T, Q8, kShort, 16, kWarp>(a, p, io, st);
-    else if (p.warps > 1) scan_launch<DIR, T, Q8, kLong, 32, kBlock>(a, p, io, st);
-    else {
+    if (p.g < 32) {
+        const auto go = [&](auto acc) {
+            if (p.g == 1) scan_launch<DIR, T, Q8, decltype(acc)::value, 1, kWarp>(a, p, io, st);
+            else if (p.g == 4) scan_launch<DIR, T, Q8, decltype(acc)::value, 4, kWarp>(a, p, io, st);
+            else scan_launch<DIR, T, Q8, decltype(acc)::value, 16, kWarp>(a, p, io, st);
+        };
+        if (vec) go(std::integral_constant<int, kVector>{});
+        else go(std::integral_constant<int, kStraight>{});
+    } else if (p.warps > 1) {
+        scan_launch<DIR, T, Q8, kRing, 32, kBlock>(a, p, io, st);
+    } else {
         if (p.parts > 1) {
-            scan_launch<DIR, T, Q8, kLong, 32, kJoin>(a, p, io, st);
+            scan_launch<DIR, T, Q8, kRing, 32, kJoin>(a, p, io, st);
             const int rc = launched(1, name);
             if (rc) return rc;
         }
-        scan_launch<DIR, T, Q8, kLong, 32, kWarp>(a, p, io, st);
+        scan_launch<DIR, T, Q8, kRing, 32, kWarp>(a, p, io, st);
     }
     return launched(1, name);
 }
@@ -100,7 +104,7 @@ template <int DIR, typename IO>
 int scan_any(const ScanArgs& a, const ScanPlan& p, const IO& io, int dtype, bool q8, bool vec, cudaStream_t st) {
     const auto go = [&](auto type, auto kept) {
         using T = decltype(type);
-        return vec ? scan_run<DIR, T, decltype(kept)::value, true>(a, p, io, st) : scan_run<DIR, T, decltype(kept)::value, false>(a, p, io, st);
+        return scan_run<DIR, T, decltype(kept)::value>(a, p, io, vec, st);
     };
     if (dtype == TCONV_F32) return q8 ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});
     return q8 ? go(__nv_bfloat16{}, std::true_type{}) : go(__nv_bfloat16{}, std::false_type{});
