@@ -17,10 +17,10 @@ constexpr int kScanChunk = 256;      // positions per warp and step; between two
 constexpr int kScanWarps = 8;        // most warps of a block on one row
 constexpr int kScanParts = 256;      // most parts of a row
 
-// How a thread's positions are read and written.  kRing: chunk by chunk through shared memory, two chunks ahead, in whole
-// 16-byte vectors whatever the rows' alignment (see Ring).  Rows of at most 128 positions: whole vectors where every row starts
-// on 16 bytes (kVector), value by value elsewhere (kStraight).
-enum ScanAccess { kVector, kStraight, kRing };
+// How a thread's positions are read and written.  Long rows go chunk by chunk through shared memory, two chunks ahead: in whole
+// 16-byte vectors where every row of every tensor starts on 16 bytes (kAligned), in words elsewhere (kWords; see Ring).  Rows of
+// at most 128 positions: whole vectors (kVector), or value by value (kStraight).
+enum ScanAccess { kVector, kStraight, kAligned, kWords };
 
 struct ScanArgs {
     int64_t rows;
@@ -138,66 +138,66 @@ template <typename T, int ACC> __device__ __forceinline__ void put_eight(T* __re
     }
 }
 
-// Four words from word S of w on, shifted down by `bits` (0 or 16) across them.
-template <int S, int N> __device__ __forceinline__ uint4 four_words(const uint32_t (&w)[N], uint32_t bits) {
-    return make_uint4(__funnelshift_r(w[S], w[S + 1], bits), __funnelshift_r(w[S + 1], w[S + 2], bits),
-                      __funnelshift_r(w[S + 2], w[S + 3], bits), S + 4 < N ? __funnelshift_r(w[S + 3], w[S + 4 < N ? S + 4 : 0], bits) : w[S + 3]);
-}
-// 16 bytes that start `shift` bytes (the same in the whole warp) into the 32 of lo and hi.
-__device__ __forceinline__ uint4 across(uint4 lo, uint4 hi, uint32_t shift) {
-    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, bits = (shift & 2) * 8;
-    switch (shift >> 2) {
-        case 0: return four_words<0>(w, bits);
-        case 1: return four_words<1>(w, bits);
-        case 2: return four_words<2>(w, bits);
-        default: return four_words<3>(w, bits);
-    }
-}
+// A warp's chunks of one row on their way through shared memory.  kWords: copied word by word from the one that holds the first
+// value on, so that only the half word of a 16-bit row with an odd start is left to be shifted out (its first word starts in
+// front of the chunk, its last one is copied up to the chunk's end).
+template <typename T, int ACC> struct Ring {
+    static constexpr bool kVec = ACC == kAligned;
+    static constexpr int kBytes = kScanChunk * (int)sizeof(T), kSlot = kBytes + 16, kSlots = 2, kUnit = kVec ? 16 : 4;
+    const char* next;                // this lane's place in the next chunk to be copied
+    uint32_t slots;                  // shared address of slot 0
+    uint32_t odd;                    // 16, or 0: bits to be shifted out
 
-// A warp's chunks of one row on their way through shared memory.  The copies are those of the aligned 16-byte vectors that hold
-// the chunk: they start up to 15 bytes before it and end as far behind it (always within 16 bytes that hold some value of the
-// row), and the values are taken out of neighbouring vectors by a shift that the whole row shares.
-template <typename T> struct Ring {
-    static constexpr int kBytes = kScanChunk * (int)sizeof(T), kVectors = kBytes / 16, kSlot = kBytes + 16, kSlots = 2;
-    const char* from;                // the row's start, rounded down
-    uint32_t shift, live;            // its distance from there in bytes; the positions to be read
-    char* slots;
-    __device__ __forceinline__ Ring(const T* row, uint32_t live, char* to)
-        : from(reinterpret_cast<const char*>(row) - (reinterpret_cast<uintptr_t>(row) & 15)),
-          shift((uint32_t)reinterpret_cast<uintptr_t>(row) & 15), live(live), slots(to) {}
-    __device__ __forceinline__ static void copy(char* to, const char* src, uint32_t bytes) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(src), "r"(bytes) : "memory");
+    __device__ __forceinline__ Ring(const T* row, uint32_t chunk, const char* to) {
+        const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>(row) & (kUnit - 1);
+        odd = !kVec && sizeof(T) == 2 ? at * 8 : 0;
+        next = reinterpret_cast<const char*>(row) - (sizeof(T) == 2 && !kVec ? at : 0) + (int64_t)chunk * kBytes + kUnit * (threadIdx.x & 31);
+        slots = (uint32_t)__cvta_generic_to_shared(to);
     }
-    // Starts the copies of a chunk; what lies behind the row's length becomes zero.
-    __device__ __forceinline__ void fetch(uint32_t chunk, int slot) {
-        const uint32_t lane = threadIdx.x & 31;
-        const char* src = from + (int64_t)chunk * kBytes;
-        char* to = slots + slot * kSlot;
-        if ((chunk + 1) * kScanChunk <= live) {
+    __device__ __forceinline__ static void copy(uint32_t to, const char* src, uint32_t bytes) {
+        if constexpr (kVec) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(bytes) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(src), "r"(bytes) : "memory");
+    }
+    __device__ __forceinline__ static void copy(uint32_t to, const char* src) {
+        if constexpr (kVec) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(src) : "memory");
+    }
+    __device__ __forceinline__ void move(int64_t bytes) { next += bytes; }
+    // Starts the copies of the chunk that `next` is at, all of it (WHOLE) or its first `count` values with zeros behind them.
+    template <bool WHOLE> __device__ __forceinline__ void fetch(int slot, uint32_t count = kScanChunk) const {
+        const uint32_t lane = threadIdx.x & 31, to = slots + slot * kSlot + kUnit * lane;
+        if constexpr (WHOLE) {
 #pragma unroll
-            for (int j = 0; j < kVectors / 32; ++j) copy(to + 16 * (32 * j + lane), src + 16 * (32 * j + lane), 16);
-            if (shift && lane == 0) copy(to + kBytes, src + kBytes, shift);
+            for (int j = 0; j < kBytes / (32 * kUnit); ++j) copy(to + 32 * kUnit * j, next + 32 * kUnit * j);
+            if (odd && lane == 0) copy(to + kBytes, next + kBytes, 2);
         } else {
-            const uint32_t first = chunk * kScanChunk, left = first < live ? shift + (live - first) * (uint32_t)sizeof(T) : 0;
+            const uint32_t left = count * (uint32_t)sizeof(T) + odd / 8;
+            const char* start = next - kUnit * lane;
 #pragma unroll
-            for (int j = 0; j < kVectors / 32 + 1; ++j) {
-                const uint32_t b = 16 * (32 * j + lane);
-                if (j == kVectors / 32 && lane) break;
-                const uint32_t n = b < left ? min(left - b, 16u) : 0;
-                copy(to + b, n ? src + b : from, n);
+            for (int j = 0; j < kBytes / (32 * kUnit); ++j) {
+                const uint32_t b = kUnit * lane + 32 * kUnit * j, n = b < left ? min(left - b, (uint32_t)kUnit) : 0;
+                copy(to + 32 * kUnit * j, n ? start + b : start, n);
+            }
+            if (lane == 0) {
+                const uint32_t n = kBytes < left ? left - kBytes : 0;
+                if (odd) copy(to + kBytes, n ? start + kBytes : start, n);
             }
         }
     }
     // This lane's eight values of a chunk that has arrived.
     __device__ __forceinline__ void take(int slot, float (&v)[8]) const {
-        const uint4* p = reinterpret_cast<const uint4*>(slots + slot * kSlot) + (threadIdx.x & 31) * Words<T>::n;
+        const uint32_t from = slots + slot * kSlot + (threadIdx.x & 31) * kScanVec * (uint32_t)sizeof(T);
         Words<T> r;
 #pragma unroll
-        for (int j = 0; j < Words<T>::n; ++j) r.w[j] = p[j];
-        if (shift) {
-            const uint4 next = p[Words<T>::n];
-#pragma unroll
-            for (int j = 0; j < Words<T>::n; ++j) r.w[j] = across(r.w[j], j + 1 < Words<T>::n ? r.w[j + 1] : next, shift);
+        for (int j = 0; j < Words<T>::n; ++j)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[j].x), "=r"(r.w[j].y), "=r"(r.w[j].z), "=r"(r.w[j].w) : "r"(from + 16 * j) : "memory");
+        if constexpr (!kVec && sizeof(T) == 2) {
+            if (odd) {
+                uint32_t last;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(last) : "r"(from + 16) : "memory");
+                uint4& w = r.w[0];
+                w = make_uint4(__funnelshift_r(w.x, w.y, 16), __funnelshift_r(w.y, w.z, 16), __funnelshift_r(w.z, w.w, 16), __funnelshift_r(w.w, last, 16));
+            }
         }
         unpack(r, v);
     }
@@ -208,42 +208,50 @@ __device__ __forceinline__ void ring_wait() {      // all but the newest group a
     __syncwarp();
 }
 
-// Writes a warp's chunk below `end`, in whole vectors: those of an unaligned row are put together across lanes in `stage`, and what
-// is left of the first and the last (16 bytes in all) goes value by value.
-template <typename T> __device__ __forceinline__ void put_chunk(T* __restrict__ row, uint32_t chunk, uint32_t end, const float (&v)[8], char* stage) {
-    constexpr int kPer = Words<T>::per;
-    const uint32_t lane = threadIdx.x & 31, first = chunk * kScanChunk;
-    if (first >= end) return;
-    T* to = row + first;
-    const uint32_t shift = (uint32_t)reinterpret_cast<uintptr_t>(to) & 15;
-    const bool whole = first + kScanChunk <= end;
+// Writes a warp's chunk at `to`, all of it (WHOLE) or its first `count` values.  16-bit rows that do not start on 16 bytes: shifted to
+// words by the half word that an odd start leaves over, laid out in `stage` as in memory, and written in whole vectors, with what
+// is left of the first and the last (16 bytes in all) value by value.  fp32 rows: word by word, a lane next to the other.
+template <typename T, int ACC, bool WHOLE>
+__device__ __forceinline__ void put_chunk(T* __restrict__ to, uint32_t count, const float (&v)[8], char* stage) {
+    const uint32_t lane = threadIdx.x & 31;
     Words<T> r;
     pack(v, r);
-    if (whole && !shift) {
+    if constexpr (ACC == kAligned) {
+#pragma unroll
+        for (int j = 0; j < Words<T>::n; ++j)
+            if (WHOLE || kScanVec * lane + j * Words<T>::per < count) reinterpret_cast<uint4*>(to)[Words<T>::n * lane + j] = r.w[j];
+        return;
+    }
+    const T* values = reinterpret_cast<const T*>(stage);
+    const uint32_t at = ((uint32_t)reinterpret_cast<uintptr_t>(to) & 15) / (uint32_t)sizeof(T);      // values into a vector
+    if (WHOLE && at == 0) {
 #pragma unroll
         for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(to)[Words<T>::n * lane + j] = r.w[j];
         return;
     }
-    uint4* s = reinterpret_cast<uint4*>(stage);
-    const T* values = reinterpret_cast<const T*>(stage);
     __syncwarp();
-#pragma unroll
-    for (int j = 0; j < Words<T>::n; ++j) s[Words<T>::n * lane + j] = r.w[j];
-    __syncwarp();
-    if (whole) {
-        uint4* aligned = reinterpret_cast<uint4*>(reinterpret_cast<char*>(to) - shift);
-#pragma unroll
-        for (int j = 0; j < Words<T>::n; ++j) {
-            const uint32_t q = 32 * j + lane;
-            const uint4 lo = s[q ? q - 1 : 0], w = across(lo, s[q], 16 - shift);
-            if (q) aligned[q] = w;
+    if constexpr (WHOLE && sizeof(T) == 2) {
+        uint4 w = r.w[0];
+        if (at & 1) {
+            const uint32_t before = __shfl_up_sync(~0u, w.w, 1);
+            if (lane == 31) reinterpret_cast<uint16_t*>(stage)[at + kScanChunk - 1] = (uint16_t)(w.w >> 16);
+            w = make_uint4(__funnelshift_l(before, w.x, 16), __funnelshift_l(w.x, w.y, 16), __funnelshift_l(w.y, w.z, 16), __funnelshift_l(w.z, w.w, 16));
         }
-        const uint32_t e = lane + shift / (uint32_t)sizeof(T) < kPer ? lane : kScanChunk - kPer + lane;
-        if (lane < kPer) to[e] = values[e];
+        uint32_t* p = reinterpret_cast<uint32_t*>(stage) + at / 2 + 4 * lane;
+        p[0] = w.x; p[1] = w.y; p[2] = w.z; p[3] = w.w;
+        __syncwarp();
+        if (lane) reinterpret_cast<uint4*>(to - at)[lane] = reinterpret_cast<const uint4*>(stage)[lane];
+        const uint32_t e = lane + at < kScanVec ? lane : kScanChunk - kScanVec + lane;
+        if (lane < kScanVec) to[e] = values[at + e];
     } else {
 #pragma unroll
+        for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(stage)[Words<T>::n * lane + j] = r.w[j];
+        __syncwarp();
+        const T* from = values + lane;
+        T* p = to + lane;
+#pragma unroll
         for (int i = 0; i < kScanVec; ++i)
-            if (first + 32 * i + lane < end) to[32 * i + lane] = values[32 * i + lane];
+            if (WHOLE || 32 * i + lane < count) p[32 * i] = from[32 * i];
     }
 }
 
@@ -300,13 +308,16 @@ template <bool UP> __device__ __forceinline__ void block_carry(const Map (&share
 // that only leaves the part's maps.
 enum ScanMode { kWarp, kBlock, kJoin };
 
+// The warp's number, in a form that the compiler knows to be the same in all lanes.
+__device__ __forceinline__ int warp_of_block() { return __shfl_sync(~0u, (int)(threadIdx.x >> 5), 0); }
+
 // Where a warp works.
 template <int G, int MODE> struct Place {
     int64_t row;
     uint32_t part;
     bool mine, any;                  // this lane's row exists; some row of the warp does
     __device__ __forceinline__ Place(const ScanArgs& a) {
-        const int warp = threadIdx.x >> 5;
+        const int warp = warp_of_block();
         if constexpr (MODE == kBlock) {
             row = blockIdx.x;
             part = 0;
@@ -322,9 +333,9 @@ template <int G, int MODE> struct Place {
     }
 };
 
-// Shared memory of a warp: rings, and a chunk to be written.
-template <typename T> __host__ __device__ constexpr int scan_space(int rings, bool writes) {
-    return rings * Ring<T>::kSlots * Ring<T>::kSlot + (writes ? Ring<T>::kBytes : 0);
+// Shared memory of a warp: rings, and a chunk to be written (with what lies beside it in its first and last vector).
+template <typename T, int ACC> __host__ __device__ constexpr int scan_space(int rings, bool writes) {
+    return rings * Ring<T, ACC>::kSlots * Ring<T, ACC>::kSlot + (writes && ACC == kWords ? Ring<T, ACC>::kBytes + 16 : 0);
 }
 
 // Forward.
@@ -333,7 +344,8 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
                                                                                           const __grid_constant__ ScanFwd io) {
     extern __shared__ __align__(16) char ring_space[];        // a warp's: slots of x, of gate, and a chunk to be written
     __shared__ Map shared[MODE == kBlock ? 2 : 1][kScanWarps], shared_q[MODE == kBlock && Q8 ? 2 : 1][kScanWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = MODE == kBlock ? blockDim.x >> 5 : 1, sub = lane % G;
+    constexpr bool kChunks = ACC == kAligned || ACC == kWords;
+    const int lane = threadIdx.x & 31, warp = warp_of_block(), warps = MODE == kBlock ? blockDim.x >> 5 : 1, sub = lane % G;
     const Place<G, MODE> at_row(a);
     if (!at_row.any) return;
     const int64_t row = at_row.row, n = row / a.C, c = row - n * a.C;
@@ -343,7 +355,9 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
     T* py = (T*)io.y + row * a.L;
     const uint32_t k_begin = G == 32 && MODE != kBlock ? at_row.part * a.per_part : 0;
     const uint32_t k_end = G == 32 && MODE != kBlock ? min(k_begin + a.per_part, a.chunks) : a.chunks;
-    const int64_t pitch = q8_pitch(a.L), nb = q8_blocks(a.L);
+    const uint32_t pitch = (uint32_t)q8_pitch(a.L);
+    const int64_t codes_at = row * pitch, scales_at = row * q8_blocks(a.L);
+    float* states = io.states ? io.states + row * a.chunks : nullptr;
 
     Map total{1.0f, 0.0f}, total_q = total;                   // kJoin: the part's maps so far
     float h = 0.0f, hq;
@@ -358,40 +372,31 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
                 if constexpr (Q8) hq = apply(warp_join({m.z, m.w}), hq);
             }
     }
-    constexpr bool kChunks = ACC == kRing;
-    using R = Ring<T>;
-    char* space = ring_space + (kChunks ? warp * scan_space<T>(2, MODE != kJoin) : 0);
-    R rx(px, end, space), rg(pg, end, space + R::kSlots * R::kSlot);
+    using R = Ring<T, ACC>;
+    char* space = ring_space + (kChunks ? warp * scan_space<T, ACC>(2, MODE != kJoin) : 0);
+    const uint32_t mine_first = k_begin + (MODE == kBlock ? warp : 0);
+    R rx(px, mine_first, space), rg(pg, mine_first, space + R::kSlots * R::kSlot);
     char* stage = space + 2 * R::kSlots * R::kSlot;
-    const auto fetch = [&](uint32_t k, int slot) {
+    // chunks of which every position is to be read; of which some are
+    const uint32_t whole = end / kScanChunk, some = (end + kScanChunk - 1) / kScanChunk;
+    const auto fetch = [&](uint32_t k, int slot) {            // (k goes up by `warps` from call to call)
         const uint32_t chunk = k + (MODE == kBlock ? warp : 0);
-        if (k < k_end && chunk * kScanChunk < end) {
-            rx.fetch(chunk, slot);
-            rg.fetch(chunk, slot);
+        if (k < k_end) {
+            if (chunk < whole) {
+                rx.template fetch<true>(slot);
+                rg.template fetch<true>(slot);
+            } else if (chunk < some) {
+                rx.template fetch<false>(slot, end - chunk * kScanChunk);
+                rg.template fetch<false>(slot, end - chunk * kScanChunk);
+            }
+            rx.move((int64_t)warps * R::kBytes);
+            rg.move((int64_t)warps * R::kBytes);
         }
         ring_commit();
     };
-    if constexpr (kChunks) {
-        fetch(k_begin, 0);
-        fetch(k_begin + warps, 1);
-    }
     int turn = 0;
-    for (uint32_t k = k_begin; k < k_end; k += warps, turn ^= 1) {
+    const auto step = [&]<bool WHOLE>(uint32_t k) {
         const uint32_t chunk = k + (MODE == kBlock ? warp : 0), here = chunk * kScanChunk + sub * kScanVec;
-        if (kChunks && MODE != kBlock && chunk * kScanChunk >= end) {      // behind the row's length, with all that follows
-            if constexpr (MODE == kJoin) break;
-            else {
-                const float zero[8] = {};
-                put_chunk(py, chunk, L, zero, stage);
-                if (io.states && sub == 0) io.states[row * a.chunks + chunk] = Q8 ? hq : h;
-                if constexpr (Q8)
-                    if (here < (uint32_t)pitch) {
-                        *reinterpret_cast<uint2*>(io.xc + row * pitch + here) = *reinterpret_cast<uint2*>(io.gc + row * pitch + here) = make_uint2(0, 0);
-                        if (here % kQ8Block == 0) io.xs[row * nb + here / kQ8Block] = io.gs[row * nb + here / kQ8Block] = 1;
-                    }
-                continue;
-            }
-        }
         float x[8], g[8], f[8], b[8];
         if constexpr (kChunks) {
             ring_wait();
@@ -403,28 +408,23 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
             get_eight<T, ACC>(px, here, end, x);
             get_eight<T, ACC>(pg, here, end, g);
         }
-        const int live = end <= here ? 0 : (int)min(end - here, (uint32_t)kScanVec);
-        if constexpr (Q8) {                                   // what lies behind the row's length is no part of a block
-            if (live < 8)
+        const int live = WHOLE ? 8 : end <= here ? 0 : (int)min(end - here, (uint32_t)kScanVec);
+        if constexpr (Q8 && !WHOLE) {                         // what lies behind the row's length is no part of a block
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i >= live) x[i] = g[i] = 0.0f;
+            for (int i = 0; i < 8; ++i)
+                if (i >= live) x[i] = g[i] = 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const Gate q = gate_of(g[i]);
             f[i] = q.f;
             b[i] = __fmul_rn(q.u, x[i]);
-        }
-        if (live < 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i >= live) { f[i] = 1.0f; b[i] = 0.0f; }
+            if (!WHOLE && i >= live) { f[i] = 1.0f; b[i] = 0.0f; }
         }
         Map m{f[0], b[0]};
 #pragma unroll
         for (int i = 1; i < 8; ++i) m = then(m, {f[i], b[i]});
-        Map all, all_q, before;
+        [[maybe_unused]] Map all, all_q, before;
         if constexpr (MODE == kJoin) all = warp_join(m);
         else {
             before = before_me<G, true>(m, all);
@@ -434,28 +434,22 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
             const uint32_t bx = block_scale<G>(x), bg = block_scale<G>(g);
             const uint2 cx = encode_eight(x, bx), cg = encode_eight(g, bg);
             if constexpr (MODE != kJoin) {
-                if (mine && here < (uint32_t)pitch) {
-                    *reinterpret_cast<uint2*>(io.xc + row * pitch + here) = cx;
-                    *reinterpret_cast<uint2*>(io.gc + row * pitch + here) = cg;
-                    if (here % kQ8Block == 0) {
-                        io.xs[row * nb + here / kQ8Block] = (uint8_t)bx;
-                        io.gs[row * nb + here / kQ8Block] = (uint8_t)bg;
+                if (WHOLE || (mine && here < pitch)) {
+                    *reinterpret_cast<uint2*>(io.xc + codes_at + here) = cx;
+                    *reinterpret_cast<uint2*>(io.gc + codes_at + here) = cg;
+                    if (sub % 4 == 0) {
+                        io.xs[scales_at + here / kQ8Block] = (uint8_t)bx;
+                        io.gs[scales_at + here / kQ8Block] = (uint8_t)bg;
                     }
                 }
             }
             Map mq{1.0f, 0.0f};
-            if (live == 8) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const Gate q = gate_of(g[i]);
-                    mq = then(mq, {q.f, __fmul_rn(q.u, x[i])});
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const Gate q = gate_of(g[i]);
-                    if (i < live) mq = then(mq, {q.f, __fmul_rn(q.u, x[i])});
-                }
+            for (int i = 0; i < 8; ++i) {
+                const Gate q = gate_of(g[i]);
+                const Map one{q.f, __fmul_rn(q.u, x[i])};
+                if (WHOLE) mq = i ? then(mq, one) : one;
+                else if (i < live) mq = then(mq, one);
             }
             if constexpr (G == 32) all_q = warp_join(mq);
             else {
@@ -480,22 +474,41 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
                 h = apply(all, h);
                 if constexpr (Q8) hq = apply(all_q, hq);
             }
-            if (io.states && mine && sub == 0 && chunk < a.chunks) io.states[row * a.chunks + chunk] = Q8 ? start_q : start;
+            if (states && sub == 0 && (WHOLE || (mine && chunk < a.chunks))) states[chunk] = Q8 ? start_q : start;
             float v = apply(before, start);
             float y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 v = fmaf(f[i], v, b[i]);
-                y[i] = v;
+                y[i] = WHOLE || i < live ? v : 0.0f;
             }
-            if (live < 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i >= live) y[i] = 0.0f;
-            }
-            if constexpr (kChunks) put_chunk(py, chunk, L, y, stage);
-            else put_eight<T, ACC>(py, here, L, y);
+            if constexpr (!kChunks) put_eight<T, ACC>(py, here, L, y);
+            else if (WHOLE || chunk < a.chunks) put_chunk<T, ACC, WHOLE>(py + (int64_t)chunk * kScanChunk, L - chunk * kScanChunk, y, stage);
         }
+        turn ^= 1;
+    };
+    uint32_t k = k_begin;
+    if constexpr (kChunks) {
+        fetch(k, 0);
+        fetch(k + warps, 1);
+    }
+    if constexpr (kChunks && MODE != kBlock) {
+        for (; k < min(k_end, whole); ++k) step.template operator()<true>(k);
+        if (k < min(k_end, some)) step.template operator()<false>(k++);
+        if constexpr (MODE != kJoin)
+            for (; k < k_end; ++k) {                          // behind the row's length
+                const float zero[8] = {};
+                const uint32_t here = k * kScanChunk + sub * kScanVec;
+                put_chunk<T, ACC, false>(py + (int64_t)k * kScanChunk, L - k * kScanChunk, zero, stage);
+                if (states && lane == 0) states[k] = Q8 ? hq : h;
+                if constexpr (Q8)
+                    if (here < pitch) {
+                        *reinterpret_cast<uint2*>(io.xc + codes_at + here) = *reinterpret_cast<uint2*>(io.gc + codes_at + here) = make_uint2(0, 0);
+                        if (sub % 4 == 0) io.xs[scales_at + here / kQ8Block] = io.gs[scales_at + here / kQ8Block] = 1;
+                    }
+            }
+    } else {
+        for (; k < k_end; k += warps) step.template operator()<false>(k);
     }
     if constexpr (kChunks) asm volatile("cp.async.wait_all;" ::: "memory");
     if constexpr (MODE == kJoin) {
@@ -512,7 +525,8 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
                                                                                           const __grid_constant__ ScanBwd io) {
     extern __shared__ __align__(16) char ring_space[];        // a warp's: slots of grad_y and, not kept in 8 bits, gate and x; a chunk
     __shared__ Map shared[MODE == kBlock ? 2 : 1][kScanWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = MODE == kBlock ? blockDim.x >> 5 : 1, sub = lane % G;
+    constexpr bool kChunks = ACC == kAligned || ACC == kWords;
+    const int lane = threadIdx.x & 31, warp = warp_of_block(), warps = MODE == kBlock ? blockDim.x >> 5 : 1, sub = lane % G;
     const Place<G, MODE> at_row(a);
     if (!at_row.any) return;
     const int64_t row = at_row.row, n = row / a.C, c = row - n * a.C;
@@ -522,9 +536,8 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
     T *ox = (T*)io.gx + n * a.ob + c * (int64_t)a.L, *og = (T*)io.gg + n * a.ob + c * (int64_t)a.L;
     const uint32_t k_begin = G == 32 && MODE != kBlock ? at_row.part * a.per_part : 0;
     const uint32_t k_end = G == 32 && MODE != kBlock ? min(k_begin + a.per_part, a.chunks) : a.chunks;
-    const int64_t pitch = q8_pitch(a.L), nb = q8_blocks(a.L);
-    const int8_t *xc = io.xc + row * pitch, *gc = io.gc + row * pitch;
-    const uint8_t *xs = io.xs + row * nb, *gs = io.gs + row * nb;
+    const int64_t codes_at = row * q8_pitch(a.L), scales_at = row * q8_blocks(a.L);
+    const float* states = io.states + row * a.chunks;
 
     Map total{1.0f, 0.0f};
     float E = 0.0f;
@@ -537,70 +550,72 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
                 E = apply(warp_join({m.x, m.y}), E);
             }
     }
-    constexpr bool kChunks = ACC == kRing;
     constexpr int kRings = Q8 ? 1 : MODE == kJoin ? 2 : 3;
-    using R = Ring<T>;
-    char* space = ring_space + (kChunks ? warp * scan_space<T>(kRings, MODE != kJoin) : 0);
-    R ry(py, end, space), rg(pg, end, space + R::kSlots * R::kSlot), rx(px, end, space + 2 * R::kSlots * R::kSlot);
+    using R = Ring<T, ACC>;
+    char* space = ring_space + (kChunks ? warp * scan_space<T, ACC>(kRings, MODE != kJoin) : 0);
     char* stage = space + kRings * R::kSlots * R::kSlot;
-    const uint32_t steps = (k_end - k_begin + warps - 1) / warps;
     // step j works on the chunks from k_begin + j * warps on; from the last step down
+    const uint32_t steps = (k_end - k_begin + warps - 1) / warps;
     const auto chunk_of = [&](uint32_t j) { return k_begin + j * warps + (MODE == kBlock ? warp : 0); };
-    const auto fetch = [&](uint32_t j, int slot) {            // (j wraps below zero: beyond steps)
-        if (j < steps && chunk_of(j) * kScanChunk < end) {
-            ry.fetch(chunk_of(j), slot);
-            if constexpr (!Q8) {
-                rg.fetch(chunk_of(j), slot);
-                if constexpr (MODE != kJoin) rx.fetch(chunk_of(j), slot);
+    const uint32_t whole = end / kScanChunk, some = (end + kScanChunk - 1) / kScanChunk;
+    uint32_t j = steps - 1;
+    if constexpr (kChunks && MODE != kBlock) {                // chunks behind the row's length
+        for (; j < steps && chunk_of(j) >= some; --j) {
+            if constexpr (MODE != kJoin) {
+                const float zero[8] = {};
+                put_chunk<T, ACC, false>(ox + (int64_t)chunk_of(j) * kScanChunk, L - chunk_of(j) * kScanChunk, zero, stage);
+                put_chunk<T, ACC, false>(og + (int64_t)chunk_of(j) * kScanChunk, L - chunk_of(j) * kScanChunk, zero, stage);
             }
+        }
+    }
+    R ry(py, chunk_of(j), space), rg(pg, chunk_of(j), space + R::kSlots * R::kSlot), rx(px, chunk_of(j), space + 2 * R::kSlots * R::kSlot);
+    const auto fetch = [&](uint32_t i, int slot) {            // (i goes down from call to call, and wraps below zero: beyond steps)
+        if (i < steps) {
+            const uint32_t chunk = chunk_of(i);
+            if (chunk < whole) {
+                ry.template fetch<true>(slot);
+                if constexpr (!Q8) rg.template fetch<true>(slot);
+                if constexpr (!Q8 && MODE != kJoin) rx.template fetch<true>(slot);
+            } else if (chunk < some) {
+                const uint32_t count = end - chunk * kScanChunk;
+                ry.template fetch<false>(slot, count);
+                if constexpr (!Q8) rg.template fetch<false>(slot, count);
+                if constexpr (!Q8 && MODE != kJoin) rx.template fetch<false>(slot, count);
+            }
+            ry.move(-(int64_t)warps * R::kBytes);
+            if constexpr (!Q8) rg.move(-(int64_t)warps * R::kBytes);
+            if constexpr (!Q8 && MODE != kJoin) rx.move(-(int64_t)warps * R::kBytes);
         }
         ring_commit();
     };
     uint2 cx, cg;
     uint32_t bx, bg;
     float state;
-    const auto fetch_kept = [&](uint32_t j) {
-        const uint32_t at = chunk_of(j) * kScanChunk + sub * kScanVec;
+    const auto fetch_kept = [&](uint32_t i) {
+        const uint32_t chunk = chunk_of(i), at = chunk * kScanChunk + sub * kScanVec;
         if constexpr (Q8) {
             cx = cg = make_uint2(0, 0);
             bx = bg = 1;
             if (at < end) {
-                cg = __ldg(reinterpret_cast<const uint2*>(gc + at));
-                bg = __ldg(gs + at / kQ8Block);
+                cg = __ldg(reinterpret_cast<const uint2*>(io.gc + codes_at + at));
+                bg = __ldg(io.gs + scales_at + at / kQ8Block);
                 if (MODE != kJoin) {
-                    cx = __ldg(reinterpret_cast<const uint2*>(xc + at));
-                    bx = __ldg(xs + at / kQ8Block);
+                    cx = __ldg(reinterpret_cast<const uint2*>(io.xc + codes_at + at));
+                    bx = __ldg(io.xs + scales_at + at / kQ8Block);
                 }
             }
         }
-        if (MODE != kJoin) state = chunk_of(j) < a.chunks ? __ldg(io.states + row * a.chunks + chunk_of(j)) : 0.0f;
+        if (MODE != kJoin) state = chunk < a.chunks ? __ldg(states + chunk) : 0.0f;
     };
-    uint32_t j = steps - 1;
-    if constexpr (kChunks && MODE != kBlock) {                // chunks behind the row's length
-        for (; j < steps && chunk_of(j) * kScanChunk >= end; --j) {
-            if constexpr (MODE != kJoin) {
-                const float zero[8] = {};
-                put_chunk(ox, chunk_of(j), L, zero, stage);
-                put_chunk(og, chunk_of(j), L, zero, stage);
-            }
-        }
-    }
-    if (j < steps) fetch_kept(j);
-    if constexpr (kChunks) {
-        fetch(j, 0);
-        fetch(j - 1, 1);
-    }
     int turn = 0;
-    for (; j < steps; --j, turn ^= 1) {
+    const auto step = [&]<bool WHOLE>() {
         const uint32_t chunk = chunk_of(j), here = chunk * kScanChunk + sub * kScanVec;
         float x[8], g[8], d[8], f[8], u[8];
         if constexpr (kChunks) {
             ring_wait();
             ry.take(turn, d);
-            if constexpr (!Q8) {
-                rg.take(turn, g);
-                if constexpr (MODE != kJoin) rx.take(turn, x);
-            }
+            if constexpr (!Q8) rg.take(turn, g);
+            if constexpr (!Q8 && MODE != kJoin) rx.take(turn, x);
             __syncwarp();
             fetch(j - 2, turn);                               // two steps ahead, into the slot just read
         } else {
@@ -614,21 +629,18 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
             decode_eight(cg, bg, g);
             if (MODE != kJoin) decode_eight(cx, bx, x);
         }
-        const float first = state;
+        [[maybe_unused]] const float first = state;
         if (kChunks && j > 0) fetch_kept(j - 1);
-        const int live = end <= here ? 0 : (int)min(end - here, (uint32_t)kScanVec);
+        const int live = WHOLE ? 8 : end <= here ? 0 : (int)min(end - here, (uint32_t)kScanVec);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const Gate q = gate_of(g[i]);
             f[i] = q.f;
             u[i] = q.u;
+            if (!WHOLE && i >= live) { f[i] = 1.0f; u[i] = 0.0f; x[i] = 0.0f; d[i] = 0.0f; }
         }
-        if (live < 8) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i >= live) { f[i] = 1.0f; u[i] = 0.0f; x[i] = 0.0f; d[i] = 0.0f; }
-        }
-        Map back{f[7], __fmul_rn(f[7], d[7])}, all;
+        [[maybe_unused]] Map all;
+        Map back{f[7], __fmul_rn(f[7], d[7])};
 #pragma unroll
         for (int i = 6; i >= 0; --i) back = {back.P * f[i], __fmul_rn(f[i], __fadd_rn(d[i], back.B))};
         if constexpr (MODE == kJoin) {
@@ -663,20 +675,31 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
                 w = __fmul_rn(f[i], D);
                 x[i] = __fmul_rn(u[i], D);
                 g[i] = __fmul_rn(__fmul_rn(w, b[i]), u[i]);
+                if (!WHOLE && i >= live) x[i] = g[i] = 0.0f;
             }
-            if (live < 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i >= live) x[i] = g[i] = 0.0f;
-            }
-            if constexpr (kChunks) {
-                put_chunk(ox, chunk, L, x, stage);
-                put_chunk(og, chunk, L, g, stage);
-            } else {
+            if constexpr (!kChunks) {
                 put_eight<T, ACC>(ox, here, L, x);
                 put_eight<T, ACC>(og, here, L, g);
+            } else if (WHOLE || chunk < a.chunks) {
+                put_chunk<T, ACC, WHOLE>(ox + (int64_t)chunk * kScanChunk, L - chunk * kScanChunk, x, stage);
+                put_chunk<T, ACC, WHOLE>(og + (int64_t)chunk * kScanChunk, L - chunk * kScanChunk, g, stage);
             }
         }
+        turn ^= 1;
+    };
+    if (j < steps) fetch_kept(j);
+    if constexpr (kChunks) {
+        fetch(j, 0);
+        fetch(j - 1, 1);
+    }
+    if constexpr (kChunks && MODE != kBlock) {
+        if (j < steps && chunk_of(j) >= whole) {
+            step.template operator()<false>();
+            --j;
+        }
+        for (; j < steps; --j) step.template operator()<true>();
+    } else {
+        for (; j < steps; --j) step.template operator()<false>();
     }
     if constexpr (kChunks) asm volatile("cp.async.wait_all;" ::: "memory");
     if constexpr (MODE == kJoin) {

@@ -70,7 +70,7 @@ void scan_launch(const ScanArgs& a, const ScanPlan& p, const IO& io, cudaStream_
         else return scan_bwd_kernel<T, Q8, ACC, G, MODE>;
     }();
     constexpr int kRings = DIR == kFwd ? 2 : Q8 ? 1 : MODE == kJoin ? 2 : 3;
-    const int warps = MODE == kBlock ? p.warps : 4, smem = ACC == kRing ? warps * scan_space<T>(kRings, MODE != kJoin) : 0;
+    const int warps = MODE == kBlock ? p.warps : 4, smem = ACC == kAligned || ACC == kWords ? warps * scan_space<T, ACC>(kRings, MODE != kJoin) : 0;
     const int64_t warps_needed = G == 32 ? a.rows * p.parts : (a.rows + 32 / G - 1) / (32 / G);
     if (smem > 48 * 1024 && allow_smem(kern, smem) != cudaSuccess) return;       // (its error is what launched() finds)
     kern<<<(unsigned)(MODE == kBlock ? a.rows : (warps_needed + 3) / 4), warps * 32, smem, st>>>(a, io);
@@ -87,15 +87,23 @@ int scan_run(const ScanArgs& a, const ScanPlan& p, const IO& io, bool vec, cudaS
         };
         if (vec) go(std::integral_constant<int, kVector>{});
         else go(std::integral_constant<int, kStraight>{});
-    } else if (p.warps > 1) {
-        scan_launch<DIR, T, Q8, kRing, 32, kBlock>(a, p, io, st);
     } else {
-        if (p.parts > 1) {
-            scan_launch<DIR, T, Q8, kRing, 32, kJoin>(a, p, io, st);
-            const int rc = launched(1, name);
-            if (rc) return rc;
-        }
-        scan_launch<DIR, T, Q8, kRing, 32, kWarp>(a, p, io, st);
+        const auto go = [&](auto acc) {
+            constexpr int ACC = decltype(acc)::value;
+            if (p.warps > 1) {
+                scan_launch<DIR, T, Q8, ACC, 32, kBlock>(a, p, io, st);
+                return 0;
+            }
+            if (p.parts > 1) {
+                scan_launch<DIR, T, Q8, ACC, 32, kJoin>(a, p, io, st);
+                const int rc = launched(1, name);
+                if (rc) return rc;
+            }
+            scan_launch<DIR, T, Q8, ACC, 32, kWarp>(a, p, io, st);
+            return 0;
+        };
+        const int rc = vec ? go(std::integral_constant<int, kAligned>{}) : go(std::integral_constant<int, kWords>{});
+        if (rc) return rc;
     }
     return launched(1, name);
 }
