@@ -101,7 +101,10 @@ __global__ void __launch_bounds__(256) q8_store_kernel(int64_t rows, int64_t inn
     const bool ok = unit < units;
     const T* px = x + (int64_t)row * inner + at;
     float v[8];
-    if constexpr (VEC) {
+    if (VEC && sizeof(T) == 4 && ok && (int64_t)at + 8 <= inner && (reinterpret_cast<uintptr_t>(px) & 31) == 0) {
+        asm volatile("ld.global.nc.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(px));
+    } else if constexpr (VEC) {
         constexpr int kWords = sizeof(T) / 2, kPer = 16 / sizeof(T);
         uint4 w[kWords];
 #pragma unroll
@@ -170,7 +173,11 @@ __global__ void __launch_bounds__(256) q8_restore_kernel(int64_t rows, int64_t i
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (float)q[i] * q8_unit(b[i]);
     }
-    if (first + 8 <= total) {
+    if (sizeof(T) == 4 && first + 8 <= total && (reinterpret_cast<uintptr_t>(x) & 31) == 0) {
+        // (two stores of 16 bytes would each reach half of every sector)
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(x + first), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                     "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+    } else if (first + 8 <= total) {
         uint32_t w[4 * kWords];
 #pragma unroll
         for (int i = 0; i < 4 * kWords; ++i) {

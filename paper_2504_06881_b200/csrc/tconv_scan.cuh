@@ -192,12 +192,10 @@ template <typename T, int ACC> struct Ring {
         for (int j = 0; j < Words<T>::n; ++j)
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[j].x), "=r"(r.w[j].y), "=r"(r.w[j].z), "=r"(r.w[j].w) : "r"(from + 16 * j) : "memory");
         if constexpr (!kVec && sizeof(T) == 2) {
-            if (odd) {
-                uint32_t last;
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(last) : "r"(from + 16) : "memory");
-                uint4& w = r.w[0];
-                w = make_uint4(__funnelshift_r(w.x, w.y, 16), __funnelshift_r(w.y, w.z, 16), __funnelshift_r(w.z, w.w, 16), __funnelshift_r(w.w, last, 16));
-            }
+            uint32_t last;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(last) : "r"(from + 16) : "memory");
+            uint4& w = r.w[0];
+            w = make_uint4(__funnelshift_r(w.x, w.y, odd), __funnelshift_r(w.y, w.z, odd), __funnelshift_r(w.z, w.w, odd), __funnelshift_r(w.w, last, odd));
         }
         unpack(r, v);
     }
@@ -208,45 +206,64 @@ __device__ __forceinline__ void ring_wait() {      // all but the newest group a
     __syncwarp();
 }
 
-// Writes a warp's chunk at `to`, all of it (WHOLE) or its first `count` values.  16-bit rows that do not start on 16 bytes: shifted to
-// words by the half word that an odd start leaves over, laid out in `stage` as in memory, and written in whole vectors, with what
-// is left of the first and the last (16 bytes in all) value by value.  fp32 rows: word by word, a lane next to the other.
+// Writes a thread's eight values to an address of whole vectors.  fp32: as 32 bytes where they start on 32, since two stores of 16
+// would each reach half of every sector.
+template <typename T> __device__ __forceinline__ void put_words(T* to, const Words<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+        if ((reinterpret_cast<uintptr_t>(to) & 31) == 0) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r.w[0].x), "r"(r.w[0].y), "r"(r.w[0].z),
+                         "r"(r.w[0].w), "r"(r.w[1].x), "r"(r.w[1].y), "r"(r.w[1].z), "r"(r.w[1].w) : "memory");
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(to)[j] = r.w[j];
+}
+
+// Four words from word S of w on, shifted down by `bits` (0 or 16) across them.
+template <int S> __device__ __forceinline__ uint4 four_words(const uint32_t (&w)[8], uint32_t bits) {
+    return make_uint4(__funnelshift_r(w[S], w[S + 1], bits), __funnelshift_r(w[S + 1], w[S + 2], bits),
+                      __funnelshift_r(w[S + 2], w[S + 3], bits), __funnelshift_r(w[S + 3], w[S + 4], bits));
+}
+// 16 bytes that start `shift` bytes (even, 2 to 14; the same in the whole warp) into the 32 of lo and hi.
+__device__ __forceinline__ uint4 across(uint4 lo, uint4 hi, uint32_t shift) {
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, bits = (shift & 2) * 8;
+    if (shift < 8) return shift < 4 ? four_words<0>(w, bits) : four_words<1>(w, bits);
+    return shift < 12 ? four_words<2>(w, bits) : four_words<3>(w, bits);
+}
+
+// Writes a warp's chunk at `to`, all of it (WHOLE) or its first `count` values.  16-bit rows that do not start on 16 bytes: in whole
+// vectors, put together from two threads' in `stage`, and what is left of the first and the last (16 bytes in all) value by
+// value.  fp32 rows: word by word, a lane next to the other.
 template <typename T, int ACC, bool WHOLE>
 __device__ __forceinline__ void put_chunk(T* __restrict__ to, uint32_t count, const float (&v)[8], char* stage) {
     const uint32_t lane = threadIdx.x & 31;
     Words<T> r;
     pack(v, r);
     if constexpr (ACC == kAligned) {
+        if constexpr (WHOLE) put_words(to + kScanVec * lane, r);
+        else
 #pragma unroll
-        for (int j = 0; j < Words<T>::n; ++j)
-            if (WHOLE || kScanVec * lane + j * Words<T>::per < count) reinterpret_cast<uint4*>(to)[Words<T>::n * lane + j] = r.w[j];
+            for (int j = 0; j < Words<T>::n; ++j)
+                if (kScanVec * lane + j * Words<T>::per < count) reinterpret_cast<uint4*>(to)[Words<T>::n * lane + j] = r.w[j];
         return;
     }
     const T* values = reinterpret_cast<const T*>(stage);
     const uint32_t at = ((uint32_t)reinterpret_cast<uintptr_t>(to) & 15) / (uint32_t)sizeof(T);      // values into a vector
     if (WHOLE && at == 0) {
-#pragma unroll
-        for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(to)[Words<T>::n * lane + j] = r.w[j];
+        put_words(to + kScanVec * lane, r);
         return;
     }
     __syncwarp();
-    if constexpr (WHOLE && sizeof(T) == 2) {
-        uint4 w = r.w[0];
-        if (at & 1) {
-            const uint32_t before = __shfl_up_sync(~0u, w.w, 1);
-            if (lane == 31) reinterpret_cast<uint16_t*>(stage)[at + kScanChunk - 1] = (uint16_t)(w.w >> 16);
-            w = make_uint4(__funnelshift_l(before, w.x, 16), __funnelshift_l(w.x, w.y, 16), __funnelshift_l(w.y, w.z, 16), __funnelshift_l(w.z, w.w, 16));
-        }
-        uint32_t* p = reinterpret_cast<uint32_t*>(stage) + at / 2 + 4 * lane;
-        p[0] = w.x; p[1] = w.y; p[2] = w.z; p[3] = w.w;
-        __syncwarp();
-        if (lane) reinterpret_cast<uint4*>(to - at)[lane] = reinterpret_cast<const uint4*>(stage)[lane];
-        const uint32_t e = lane + at < kScanVec ? lane : kScanChunk - kScanVec + lane;
-        if (lane < kScanVec) to[e] = values[at + e];
-    } else {
 #pragma unroll
-        for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(stage)[Words<T>::n * lane + j] = r.w[j];
-        __syncwarp();
+    for (int j = 0; j < Words<T>::n; ++j) reinterpret_cast<uint4*>(stage)[Words<T>::n * lane + j] = r.w[j];
+    __syncwarp();
+    if constexpr (WHOLE && sizeof(T) == 2) {
+        const uint4 w = across(reinterpret_cast<const uint4*>(stage)[lane ? lane - 1 : 0], r.w[0], 16 - 2 * at);
+        if (lane) reinterpret_cast<uint4*>(to - at)[lane] = w;
+        const uint32_t e = lane + at < kScanVec ? lane : kScanChunk - kScanVec + lane;
+        if (lane < kScanVec) to[e] = values[e];
+    } else {
         const T* from = values + lane;
         T* p = to + lane;
 #pragma unroll
@@ -262,20 +279,28 @@ __device__ __forceinline__ Map then(Map first, Map second) { return {first.P * s
 __device__ __forceinline__ float apply(Map m, float h) { return fmaf(m.P, h, m.B); }
 
 // Joins the maps of the G threads of a row in order (UP: from the first thread on): a thread gets the map of all before it;
-// `all` (valid in the last thread) is the whole group's.
+// `all` (valid in the last thread) is the whole group's.  The shuffle's own predicate says whether there is a thread that far.
 template <int G, bool UP> __device__ __forceinline__ Map before_me(Map m, Map& all) {
-    const int sub = (threadIdx.x & 31) % G, me = UP ? sub : G - 1 - sub;
+    constexpr int kBounds = ((32 - G) << 8) | (UP ? 0 : G - 1);
 #pragma unroll
     for (int d = 1; d < G; d <<= 1) {
-        const Map o{UP ? __shfl_up_sync(~0u, m.P, d, G) : __shfl_down_sync(~0u, m.P, d, G),
-                    UP ? __shfl_up_sync(~0u, m.B, d, G) : __shfl_down_sync(~0u, m.B, d, G)};
-        if (me >= d) m = then(o, m);
+        if constexpr (UP)
+            asm volatile("{.reg .pred p; .reg .f32 a, b;\n\tshfl.sync.up.b32 b|p, %1, %2, %3, 0xffffffff;\n\tshfl.sync.up.b32 a, %0, %2, %3, 0xffffffff;\n\t"
+                         "@p fma.rn.f32 %1, %0, b, %1;\n\t@p mul.rn.f32 %0, %0, a;}" : "+f"(m.P), "+f"(m.B) : "r"(d), "n"(kBounds));
+        else
+            asm volatile("{.reg .pred p; .reg .f32 a, b;\n\tshfl.sync.down.b32 b|p, %1, %2, %3, 0xffffffff;\n\tshfl.sync.down.b32 a, %0, %2, %3, 0xffffffff;\n\t"
+                         "@p fma.rn.f32 %1, %0, b, %1;\n\t@p mul.rn.f32 %0, %0, a;}" : "+f"(m.P), "+f"(m.B) : "r"(d), "n"(kBounds));
     }
     all = m;
     if constexpr (G == 1) return {1.0f, 0.0f};
-    const Map o{UP ? __shfl_up_sync(~0u, m.P, 1, G) : __shfl_down_sync(~0u, m.P, 1, G),
-                UP ? __shfl_up_sync(~0u, m.B, 1, G) : __shfl_down_sync(~0u, m.B, 1, G)};
-    return me == 0 ? Map{1.0f, 0.0f} : o;
+    Map o;
+    if constexpr (UP)
+        asm volatile("{.reg .pred p;\n\tshfl.sync.up.b32 %0|p, %2, 1, %4, 0xffffffff;\n\tshfl.sync.up.b32 %1, %3, 1, %4, 0xffffffff;\n\t"
+                     "@!p mov.f32 %0, 0f3f800000;\n\t@!p mov.f32 %1, 0f00000000;}" : "=&f"(o.P), "=&f"(o.B) : "f"(m.P), "f"(m.B), "n"(kBounds));
+    else
+        asm volatile("{.reg .pred p;\n\tshfl.sync.down.b32 %0|p, %2, 1, %4, 0xffffffff;\n\tshfl.sync.down.b32 %1, %3, 1, %4, 0xffffffff;\n\t"
+                     "@!p mov.f32 %0, 0f3f800000;\n\t@!p mov.f32 %1, 0f00000000;}" : "=&f"(o.P), "=&f"(o.B) : "f"(m.P), "f"(m.B), "n"(kBounds));
+    return o;
 }
 template <int G, bool UP> __device__ __forceinline__ Map of_last(Map all) {
     const int src = UP ? G - 1 : 0;
@@ -333,14 +358,15 @@ template <int G, int MODE> struct Place {
     }
 };
 
-// Shared memory of a warp: rings, and a chunk to be written (with what lies beside it in its first and last vector).
+// Shared memory of a warp: rings, and a chunk to be written.
 template <typename T, int ACC> __host__ __device__ constexpr int scan_space(int rings, bool writes) {
-    return rings * Ring<T, ACC>::kSlots * Ring<T, ACC>::kSlot + (writes && ACC == kWords ? Ring<T, ACC>::kBytes + 16 : 0);
+    return rings * Ring<T, ACC>::kSlots * Ring<T, ACC>::kSlot + (writes && ACC == kWords ? Ring<T, ACC>::kBytes : 0);
 }
 
 // Forward.
 template <typename T, bool Q8, int ACC, int G, int MODE>
-__global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_fwd_kernel(const __grid_constant__ ScanArgs a,
+__global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128, MODE == kWarp && G == 32 ? 7 : 1)
+scan_fwd_kernel(const __grid_constant__ ScanArgs a,
                                                                                           const __grid_constant__ ScanFwd io) {
     extern __shared__ __align__(16) char ring_space[];        // a warp's: slots of x, of gate, and a chunk to be written
     __shared__ Map shared[MODE == kBlock ? 2 : 1][kScanWarps], shared_q[MODE == kBlock && Q8 ? 2 : 1][kScanWarps];
@@ -350,7 +376,8 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
     if (!at_row.any) return;
     const int64_t row = at_row.row, n = row / a.C, c = row - n * a.C;
     const bool mine = at_row.mine;
-    const uint32_t end = mine ? row_length(a, n) : 0u, L = mine ? a.L : 0u;
+    const uint32_t length = mine ? row_length(a, n) : 0u, L = mine ? a.L : 0u;
+    const uint32_t end = G == 32 ? __shfl_sync(~0u, length, 0) : length;      // (known to be the same in all lanes)
     const T *px = (const T*)io.x + n * a.xb + c * a.xr, *pg = (const T*)io.gate + n * a.gb + c * a.gr;
     T* py = (T*)io.y + row * a.L;
     const uint32_t k_begin = G == 32 && MODE != kBlock ? at_row.part * a.per_part : 0;
@@ -508,6 +535,8 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
                     }
             }
     } else {
+        if constexpr (kChunks)                                // (all warps of the block alike: they meet in the step)
+            for (; k + warps <= whole; k += warps) step.template operator()<true>(k);
         for (; k < k_end; k += warps) step.template operator()<false>(k);
     }
     if constexpr (kChunks) asm volatile("cp.async.wait_all;" ::: "memory");
@@ -521,7 +550,8 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_f
 // Backward, from a row's end to its front: with E_t = f_t D_t, D_t = dy_t + E_{t+1}, a stretch maps the E behind it to the one in
 // front of it, E -> P E + Q, by the same P.  The states of the chunks make the recomputed h of a chunk its own affair.
 template <typename T, bool Q8, int ACC, int G, int MODE>
-__global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_bwd_kernel(const __grid_constant__ ScanArgs a,
+__global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128, MODE == kWarp && G == 32 ? 7 : 1)
+scan_bwd_kernel(const __grid_constant__ ScanArgs a,
                                                                                           const __grid_constant__ ScanBwd io) {
     extern __shared__ __align__(16) char ring_space[];        // a warp's: slots of grad_y and, not kept in 8 bits, gate and x; a chunk
     __shared__ Map shared[MODE == kBlock ? 2 : 1][kScanWarps];
@@ -531,7 +561,8 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
     if (!at_row.any) return;
     const int64_t row = at_row.row, n = row / a.C, c = row - n * a.C;
     const bool mine = at_row.mine;
-    const uint32_t end = mine ? row_length(a, n) : 0u, L = mine ? a.L : 0u;
+    const uint32_t length = mine ? row_length(a, n) : 0u, L = mine ? a.L : 0u;
+    const uint32_t end = G == 32 ? __shfl_sync(~0u, length, 0) : length;      // (known to be the same in all lanes)
     const T *px = (const T*)io.x + n * a.xb + c * a.xr, *pg = (const T*)io.gate + n * a.gb + c * a.gr, *py = (const T*)io.gy + row * a.L;
     T *ox = (T*)io.gx + n * a.ob + c * (int64_t)a.L, *og = (T*)io.gg + n * a.ob + c * (int64_t)a.L;
     const uint32_t k_begin = G == 32 && MODE != kBlock ? at_row.part * a.per_part : 0;
@@ -558,16 +589,15 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
     const uint32_t steps = (k_end - k_begin + warps - 1) / warps;
     const auto chunk_of = [&](uint32_t j) { return k_begin + j * warps + (MODE == kBlock ? warp : 0); };
     const uint32_t whole = end / kScanChunk, some = (end + kScanChunk - 1) / kScanChunk;
-    uint32_t j = steps - 1;
-    if constexpr (kChunks && MODE != kBlock) {                // chunks behind the row's length
-        for (; j < steps && chunk_of(j) >= some; --j) {
-            if constexpr (MODE != kJoin) {
-                const float zero[8] = {};
-                put_chunk<T, ACC, false>(ox + (int64_t)chunk_of(j) * kScanChunk, L - chunk_of(j) * kScanChunk, zero, stage);
-                put_chunk<T, ACC, false>(og + (int64_t)chunk_of(j) * kScanChunk, L - chunk_of(j) * kScanChunk, zero, stage);
-            }
+    // steps with something to read, where a warp works alone: those behind are a row's end, all zeros
+    const uint32_t busy = kChunks && MODE != kBlock ? min(steps, some > k_begin ? some - k_begin : 0) : steps;
+    if constexpr (kChunks && MODE == kWarp)
+        for (uint32_t i = busy; i < steps; ++i) {
+            const float zero[8] = {};
+            put_chunk<T, ACC, false>(ox + (int64_t)chunk_of(i) * kScanChunk, L - chunk_of(i) * kScanChunk, zero, stage);
+            put_chunk<T, ACC, false>(og + (int64_t)chunk_of(i) * kScanChunk, L - chunk_of(i) * kScanChunk, zero, stage);
         }
-    }
+    uint32_t j = busy - 1;                                    // (wraps where there is none)
     R ry(py, chunk_of(j), space), rg(pg, chunk_of(j), space + R::kSlots * R::kSlot), rx(px, chunk_of(j), space + 2 * R::kSlots * R::kSlot);
     const auto fetch = [&](uint32_t i, int slot) {            // (i goes down from call to call, and wraps below zero: beyond steps)
         if (i < steps) {
@@ -651,9 +681,9 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
             float b[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) b[i] = __fmul_rn(u[i], x[i]);
-            Map m{f[0], b[0]}, unused;
+            Map m{back.P, b[0]}, unused;
 #pragma unroll
-            for (int i = 1; i < 8; ++i) m = then(m, {f[i], b[i]});
+            for (int i = 1; i < 8; ++i) m.B = fmaf(f[i], m.B, b[i]);
             const Map behind = before_me<G, false>(back, all), before = before_me<G, true>(m, unused);
             all = of_last<G, false>(all);
             float start = E;
@@ -699,7 +729,9 @@ __global__ void __launch_bounds__(MODE == kBlock ? kScanWarps * 32 : 128) scan_b
         }
         for (; j < steps; --j) step.template operator()<true>();
     } else {
-        for (; j < steps; --j) step.template operator()<false>();
+        for (; j < steps && (!kChunks || (j + 1) * warps > whole); --j) step.template operator()<false>();
+        if constexpr (kChunks)                                // (all warps of the block alike: they meet in the step)
+            for (; j < steps; --j) step.template operator()<true>();
     }
     if constexpr (kChunks) asm volatile("cp.async.wait_all;" ::: "memory");
     if constexpr (MODE == kJoin) {
@@ -715,7 +747,9 @@ struct ScanPlan {
     uint32_t per_part;               // chunks
 };
 
-inline ScanPlan plan_scan(int64_t rows, int64_t L) {
+// heavy: fp32 kernels of 70 registers or so, which memory bounds (in bf16 a warp a row stays ahead: 46 us against 52 for 4096 rows of
+// 3981 positions backward).  (What a row's state is made of does not hang on it: chunk by chunk in order in any case.)
+inline ScanPlan plan_scan(int64_t rows, int64_t L, bool heavy) {
     const int64_t chunks = (L + kScanChunk - 1) / kScanChunk;
     ScanPlan p{32, 1, 1, (uint32_t)chunks};
     if (L <= 8) p.g = 1;
@@ -723,7 +757,9 @@ inline ScanPlan plan_scan(int64_t rows, int64_t L) {
     else if (L <= 128) p.g = 16;
     if (p.g < 32) return p;
     const int64_t enough = 148 * 16;     // warps that keep the GPU busy
-    if (rows * kScanWarps >= enough || chunks < 4 * kScanWarps) {
+    const int64_t fit = 148 * 28;        // heavy warps on the GPU at once: a little more of them take twice as long, shared rows do not
+    if (heavy && rows > fit && rows < 2 * fit && chunks > 1) p.warps = 2;
+    else if (rows * kScanWarps >= enough || chunks < 4 * kScanWarps) {
         while (p.warps < kScanWarps && p.warps < chunks && rows * p.warps < enough) p.warps *= 2;
     } else {
         int64_t parts = 2 * enough / rows;

@@ -41,14 +41,14 @@ template <typename F> int q8_types(Q8Rows q, int dtype, F f) {
     return small ? f(__nv_bfloat16{}, uint32_t{}) : f(__nv_bfloat16{}, int64_t{});
 }
 
-int check_scan(const tconv_scan_desc_t* d, ScanArgs* a, ScanPlan* p) {
+int check_scan(const tconv_scan_desc_t* d, ScanArgs* a, ScanPlan* p, bool heavy = false) {
     if (!d || d->N <= 0 || d->C <= 0 || d->L <= 0 || (d->dtype != TCONV_F32 && d->dtype != TCONV_BF16))
         return TCONV_ERR_INVALID_ARG;
     if (d->x_batch < 0 || d->x_row < 0 || d->gate_batch < 0 || d->gate_row < 0 || d->grad_batch < 0) return TCONV_ERR_INVALID_ARG;
     const int64_t rows = (int64_t)d->N * d->C;
     // (positions of a row are counted in 32 bits, a few chunks beyond its end among them)
     if (rows > kMost / d->L || rows > (int64_t)INT32_MAX || d->L > (int64_t)INT32_MAX) return TCONV_ERR_TOO_LARGE;
-    *p = plan_scan(rows, d->L);
+    *p = plan_scan(rows, d->L, heavy && d->dtype == TCONV_F32);
     *a = ScanArgs{rows, (uint32_t)d->L, (uint32_t)((d->L + kScanChunk - 1) / kScanChunk), p->per_part, d->C, p->parts,
                   d->x_batch, d->x_row, d->gate_batch, d->gate_row, d->grad_batch, nullptr, nullptr};
     return TCONV_OK;
@@ -239,7 +239,7 @@ int tconv_scan_forward(const tconv_scan_desc_t* desc, const void* x, const void*
                        void* workspace, size_t workspace_bytes, void* stream) {
     ScanArgs a;
     ScanPlan p;
-    const int rc = check_scan(desc, &a, &p);
+    const int rc = check_scan(desc, &a, &p, x_codes != nullptr);
     if (rc) return rc;
     const int kept = !!x_codes + !!x_scales + !!gate_codes + !!gate_scales;
     if (!x || !gate || !y || !h_last || (kept != 0 && kept != 4) || (kept && !states)) return TCONV_ERR_INVALID_ARG;
@@ -264,7 +264,7 @@ int tconv_scan_backward(const tconv_scan_desc_t* desc, const void* x, const void
                         void* workspace, size_t workspace_bytes, void* stream) {
     ScanArgs a;
     ScanPlan p;
-    const int rc = check_scan(desc, &a, &p);
+    const int rc = check_scan(desc, &a, &p, true);
     if (rc) return rc;
     const int kept = !!x_codes + !!x_scales + !!gate_codes + !!gate_scales;
     if ((kept != 4 && (kept != 0 || !x || !gate)) || !states || !grad_y || !grad_x || !grad_gate) return TCONV_ERR_INVALID_ARG;
