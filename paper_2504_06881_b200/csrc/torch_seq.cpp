@@ -1,6 +1,8 @@
 // The gated recurrence, the RMS norm and the 8-bit store in native code (see torch_layers.cpp): argument checks,
 // allocation, library calls, and autograd nodes.
 #include <ATen/TracerMode.h>
+#include <ATen/core/LegacyTypeDispatch.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/cuda/CUDAContext.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <torch/extension.h>
@@ -38,6 +40,23 @@ void same(const Tensor& t, const Tensor& like, at::ScalarType type, at::IntArray
                       " tensor of shape ", shape, " on ", like.device(), ", got ", t.scalar_type(), " ", t.sizes(), " on ",
                       t.device());
 }
+// Allocation past the dispatcher, which costs the host more than the allocator does.
+Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const Tensor& like) {
+    return Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));
+}
+Tensor bytes(size_t n, const Tensor& like) {
+    const int64_t size[1] = {(int64_t)n};
+    return n ? fresh(size, at::kByte, like) : Tensor();
+}
+// Places in a buffer, each on 256 bytes.
+struct Places {
+    size_t end = 0;
+    size_t add(size_t n) {
+        const size_t at = end;
+        end += (n + 255) / 256 * 256;
+        return at;
+    }
+};
 // t dense and aligned to 16 bytes, copied where it is not.
 Tensor dense(const Tensor& t) {
     if (!t.defined()) return t;
@@ -75,7 +94,8 @@ std::pair<int64_t, int64_t> q8_rows(at::IntArrayRef shape) {
 }
 Q8 q8_empty(const Tensor& like, int64_t rows, int64_t inner) {
     const int64_t pitch = (inner + 7) / 8 * 8, nb = (inner + 31) / 32;
-    return {at::empty({rows, pitch}, like.options().dtype(at::kChar)), at::empty({rows, nb}, like.options().dtype(at::kByte))};
+    const int64_t c[2] = {rows, pitch}, b[2] = {rows, nb};
+    return {fresh(c, at::kChar, like), fresh(b, at::kByte, like)};
 }
 void q8_check(const Q8& q, const Tensor& like, int64_t rows, int64_t inner) {
     const int64_t c[2] = {rows, (inner + 7) / 8 * 8}, s[2] = {rows, (inner + 31) / 32};
@@ -89,8 +109,8 @@ std::tuple<Tensor, Tensor> q8_store(const Tensor& x) {
     const int dt = dtype_of(x, "x");
     c10::cuda::CUDAGuard guard(x.device());
     const auto [rows, inner] = q8_rows(x.sizes());
-    at::NoGradGuard off;
-    const Tensor xc = dense(x.detach());
+    at::AutoDispatchBelowADInplaceOrView below;
+    const Tensor xc = dense(x);
     const Q8 q = q8_empty(x, rows, inner);
     if (const int rc = tconv_q8_store(rows, inner, dt, ptr(xc), ptr(q.codes), ptr(q.scales), stream())) fail(rc, "tconv_q8_store");
     return {q.codes, q.scales};
@@ -102,7 +122,7 @@ Tensor q8_restore(const Tensor& codes, const Tensor& scales, std::vector<int64_t
     const auto [rows, inner] = q8_rows(shape);
     q8_check({codes, scales}, codes, rows, inner);
     const Tensor c = dense(codes), s = dense(scales);
-    Tensor x = at::empty(shape, codes.options().dtype(dtype == TCONV_F32 ? at::kFloat : at::kBFloat16));
+    Tensor x = fresh(shape, dtype == TCONV_F32 ? at::kFloat : at::kBFloat16, codes);
     if (const int rc = tconv_q8_restore(rows, inner, dtype, ptr(c), ptr(s), ptr(x), stream())) fail(rc, "tconv_q8_restore");
     return x;
 }
@@ -110,29 +130,34 @@ Tensor q8_restore(const Tensor& codes, const Tensor& scales, std::vector<int64_t
 // ---- gated recurrence -----------------------------------------------------------------------------------------
 // x [N, C, L] and gate [N, C, L], or both in one tensor [N, 2C, L].
 struct Signals {
-    Tensor x, g;          // as the kernels read them: positions next to each other
+    Tensor x, g;          // as the kernels read them: positions next to each other (packed: x alone)
+    const void *px, *pg;
     bool packed;
-    int dt;
+    at::ScalarType type;
     tconv_scan_desc_t d;
-    at::ScalarType type() const { return x.scalar_type(); }
     int64_t rows() const { return (int64_t)d.N * d.C; }
 };
 Tensor row_dense(const Tensor& t) { return t.size(2) == 1 || t.stride(2) == 1 ? t : t.contiguous(); }
 
 Signals signals(const Tensor& x, const Tensor& gate) {
     Signals s;
-    s.dt = dtype_of(x, "x");
+    const int dt = dtype_of(x, "x");
+    s.type = x.scalar_type();
     s.packed = !gate.defined();
     TORCH_CHECK_VALUE(x.dim() == 3, "x: need a tensor of 3 dimensions, got ", x.dim());
     TORCH_CHECK_VALUE(!s.packed || x.size(1) % 2 == 0, "x: without a gate it holds as many gates as values, got ", x.size(1), " channels");
     const int64_t N = x.size(0), C = s.packed ? x.size(1) / 2 : x.size(1), L = x.size(2);
     TORCH_CHECK_VALUE(N <= INT32_MAX && C <= INT32_MAX, "a size exceeds 31 bits");
-    if (!s.packed) same(gate, x, x.scalar_type(), x.sizes(), "gate");
-    const Tensor whole = row_dense(x);
-    s.x = s.packed ? whole.narrow(1, 0, C) : whole;
-    s.g = s.packed ? whole.narrow(1, C, C) : row_dense(gate);
-    s.d = tconv_scan_desc_t{(int32_t)N, (int32_t)C, L, s.dt, s.x.stride(0), s.x.stride(1), s.g.stride(0), s.g.stride(1),
-                            (s.packed ? 2 : 1) * C * L};
+    if (!s.packed) same(gate, x, s.type, x.sizes(), "gate");
+    s.x = row_dense(x);
+    s.px = ptr(s.x);
+    if (s.packed) s.pg = (const char*)s.px + C * s.x.stride(1) * s.x.element_size();
+    else {
+        s.g = row_dense(gate);
+        s.pg = ptr(s.g);
+    }
+    const Tensor& g = s.packed ? s.x : s.g;
+    s.d = tconv_scan_desc_t{(int32_t)N, (int32_t)C, L, dt, s.x.stride(0), s.x.stride(1), g.stride(0), g.stride(1), (s.packed ? 2 : 1) * C * L};
     return s;
 }
 Tensor row_lengths(const Tensor& lengths, const Signals& s) {
@@ -146,98 +171,103 @@ Tensor row_lengths(const Tensor& lengths, const Signals& s) {
     return dense(lengths);
 }
 
+// What a backward pass needs, in one buffer: the states, and x and gate in 8 bits.
 struct ScanKept {
-    Q8 x, g;
-    Tensor states, lengths;
+    size_t states, xc, xs, gc, gs, size;
+    ScanKept(const tconv_scan_desc_t& d, bool q8) {
+        const int64_t rows = (int64_t)d.N * d.C;
+        Places p;
+        states = p.add(tconv_scan_states_bytes(&d));
+        if (q8) {
+            const size_t c = tconv_q8_codes_bytes(rows, d.L), s = tconv_q8_scales_bytes(rows, d.L);
+            xc = p.add(c);
+            xs = p.add(s);
+            gc = p.add(c);
+            gs = p.add(s);
+        }
+        size = p.end;
+    }
 };
 
-std::tuple<Tensor, Tensor> scan_forward(const Signals& s, const Tensor& h0_, const Tensor& lengths, bool keep, bool q8, ScanKept& k) {
-    const int64_t nc[2] = {s.d.N, s.d.C};
+struct ScanOut {
+    Tensor y, last, kept, lengths;
+};
+ScanOut scan_forward(const Signals& s, const Tensor& h0_, const Tensor& lengths, bool keep, bool q8) {
+    const int64_t nc[2] = {s.d.N, s.d.C}, ncl[3] = {s.d.N, s.d.C, s.d.L};
     same(h0_, s.x, at::kFloat, nc, "h0");
     const Tensor h0 = dense(h0_);
-    const auto opt = s.x.options();
-    k.lengths = row_lengths(lengths, s);
-    Tensor y = at::empty({s.d.N, s.d.C, s.d.L}, opt), last = at::empty(nc, opt.dtype(at::kFloat)), ws;
-    if (keep) k.states = at::empty({(int64_t)tconv_scan_states_bytes(&s.d) / 4}, opt.dtype(at::kFloat));
-    if (keep && q8) {
-        k.x = q8_empty(s.x, s.rows(), s.d.L);
-        k.g = q8_empty(s.x, s.rows(), s.d.L);
-    }
+    ScanOut o;
+    o.lengths = row_lengths(lengths, s);
+    const ScanKept k(s.d, q8);
+    if (keep) o.kept = bytes(k.size, s.x);
+    o.y = fresh(ncl, s.type, s.x);
+    o.last = fresh(nc, at::kFloat, s.x);
     const size_t n = tconv_scan_workspace_bytes(&s.d, 0);
-    if (n) ws = at::empty({(int64_t)n}, opt.dtype(at::kByte));
-    const int rc = tconv_scan_forward(&s.d, ptr(s.x), ptr(s.g), fptr(h0), (const int32_t*)ptr(k.lengths), ptr(y), fptr(last),
-                                      fptr(k.states), ptr(k.x.codes), ptr(k.x.scales), ptr(k.g.codes), ptr(k.g.scales), ptr(ws), n,
-                                      stream());
+    const Tensor ws = bytes(n, s.x);
+    char* b = keep ? (char*)ptr(o.kept) : nullptr;
+    const auto at_place = [&](size_t p) { return keep && q8 ? b + p : nullptr; };
+    const int rc = tconv_scan_forward(&s.d, s.px, s.pg, fptr(h0), (const int32_t*)ptr(o.lengths), ptr(o.y), fptr(o.last),
+                                      keep ? (float*)(b + k.states) : nullptr, at_place(k.xc), at_place(k.xs), at_place(k.gc), at_place(k.gs),
+                                      ptr(ws), n, stream());
     if (rc) fail(rc, "tconv_scan_forward");
-    return {y, last};
+    return o;
 }
 
 class GatedScan : public torch::autograd::Function<GatedScan> {
 public:
     static variable_list forward(AutogradContext* ctx, const Variable& x, const OptTensor& gate_, const OptTensor& h0_,
                                  const OptTensor& lengths, bool q8) {
+        at::AutoDispatchBelowADInplaceOrView below;
         const Tensor gate = given(gate_), h0 = given(h0_);
         ctx->set_materialize_grads(false);
         const Signals s = signals(x, gate);
-        ScanKept k;
-        auto [y, last] = scan_forward(s, h0, given(lengths), true, q8, k);
-        ctx->saved_data["sizes"] = std::vector<int64_t>{s.d.N, s.d.C, s.d.L, s.dt, s.packed, q8, h0.defined()};
-        if (q8)
-            ctx->save_for_backward({k.x.codes, k.x.scales, k.g.codes, k.g.scales, k.states, k.lengths});
-        else
-            ctx->save_for_backward({x, gate, k.states, k.lengths});
-        return {y, last};
+        ScanOut o = scan_forward(s, h0, given(lengths), true, q8);
+        ctx->saved_data["sizes"] = std::vector<int64_t>{s.d.N, s.d.C, s.d.L, s.d.dtype, s.packed, q8, h0.defined()};
+        if (q8) ctx->save_for_backward({o.kept, o.lengths});
+        else ctx->save_for_backward({o.kept, o.lengths, x, gate});
+        return {o.y, o.last};
     }
     static variable_list backward(AutogradContext* ctx, variable_list go) {
         once("gated_scan");
         if (!go[0].defined() && !go[1].defined()) return variable_list(5);
         const auto v = ctx->get_saved_variables();
         const auto z = ctx->saved_data["sizes"].toIntVector();
+        at::AutoDispatchBelowADInplaceOrView below;
         const int64_t N = z[0], C = z[1], L = z[2];
         const bool packed = z[4], q8 = z[5];
         const at::ScalarType type = z[3] == TCONV_F32 ? at::kFloat : at::kBFloat16;
-        const Tensor states = v[q8 ? 4 : 2], lengths = v[q8 ? 5 : 3];
-        const int64_t full[3] = {N, C, L}, nc[2] = {N, C}, nl[1] = {N};
-        TORCH_CHECK_VALUE(states.defined() && states.is_cuda(), "states: need the CUDA tensor that the forward saved");
-        c10::cuda::CUDAGuard guard(states.device());
+        const int64_t full[3] = {N, C, L}, wide[3] = {N, 2 * C, L}, nc[2] = {N, C}, nl[1] = {N};
+        TORCH_CHECK_VALUE(v[0].defined() && v[0].is_cuda(), "states: need the CUDA tensor that the forward saved");
+        c10::cuda::CUDAGuard guard(v[0].device());
         Signals s;
-        Q8 qx, qg;
         if (q8) {
-            qx = {v[0], v[1]};
-            qg = {v[2], v[3]};
-            q8_check(qx, states, N * C, L);
-            q8_check(qg, states, N * C, L);
+            s.px = s.pg = nullptr;
             s.d = tconv_scan_desc_t{(int32_t)N, (int32_t)C, L, (int32_t)z[3], 0, 0, 0, 0, (packed ? 2 : 1) * C * L};
         } else {
-            s = signals(v[0], v[1]);
-            TORCH_CHECK_VALUE(s.packed == packed && s.type() == type, "x, gate: need the tensors that the forward saved");
-            same(s.x, states, type, full, "x");
+            s = signals(v[2], v[3]);
+            TORCH_CHECK_VALUE(s.packed == packed, "x, gate: need the tensors that the forward saved");
+            same(s.x, v[0], type, packed ? at::IntArrayRef(wide) : at::IntArrayRef(full), "x");
         }
-        const int64_t sn[1] = {(int64_t)tconv_scan_states_bytes(&s.d) / 4};
-        same(states, states, at::kFloat, sn, "states");
-        same(lengths, states, at::kInt, nl, "lengths");
-        same(go[0], states, type, full, "grad_y");
-        same(go[1], states, at::kFloat, nc, "grad_h_last");
-        const auto opt = states.options().dtype(type);
-        const Tensor gy = go[0].defined() ? dense(go[0]) : at::zeros(full, opt), gh = dense(go[1]);
-        const Tensor st = dense(states), len = dense(lengths);
-        Tensor both, gx, gg, gh0, ws;
-        if (packed) {
-            both = at::empty({N, 2 * C, L}, opt);
-            gx = both.narrow(1, 0, C);
-            gg = both.narrow(1, C, C);
-        } else {
-            gx = at::empty(full, opt);
-            gg = at::empty(full, opt);
-        }
-        if (z[6]) gh0 = at::empty(nc, opt.dtype(at::kFloat));
+        const ScanKept k(s.d, q8);
+        const int64_t size[1] = {(int64_t)k.size};
+        same(v[0], v[0], at::kByte, size, "states");
+        same(v[1], v[0], at::kInt, nl, "lengths");
+        same(go[0], v[0], type, full, "grad_y");
+        same(go[1], v[0], at::kFloat, nc, "grad_h_last");
+        const Tensor kept = dense(v[0]), len = dense(v[1]), gh = dense(go[1]);
+        const Tensor gy = go[0].defined() ? dense(go[0]) : at::zeros(full, kept.options().dtype(type));
+        Tensor gx = fresh(packed ? at::IntArrayRef(wide) : at::IntArrayRef(full), type, kept), gg, gh0;
+        if (!packed) gg = fresh(full, type, kept);
+        if (z[6]) gh0 = fresh(nc, at::kFloat, kept);
         const size_t n = tconv_scan_workspace_bytes(&s.d, 1);
-        if (n) ws = at::empty({(int64_t)n}, opt.dtype(at::kByte));
-        const int rc = tconv_scan_backward(&s.d, ptr(s.x), ptr(s.g), ptr(qx.codes), ptr(qx.scales), ptr(qg.codes), ptr(qg.scales),
-                                           (const int32_t*)ptr(len), fptr(st), ptr(gy), fptr(gh), ptr(gx), ptr(gg), fptr(gh0), ptr(ws),
-                                           n, stream());
+        const Tensor ws = bytes(n, kept);
+        const char* b = (const char*)ptr(kept);
+        const auto at_place = [&](size_t p) { return q8 ? b + p : nullptr; };
+        const int rc = tconv_scan_backward(&s.d, s.px, s.pg, at_place(k.xc), at_place(k.xs), at_place(k.gc), at_place(k.gs),
+                                           (const int32_t*)ptr(len), (const float*)(b + k.states), ptr(gy), fptr(gh), ptr(gx),
+                                           packed ? (char*)ptr(gx) + C * L * gx.element_size() : ptr(gg), fptr(gh0), ptr(ws), n, stream());
         if (rc) fail(rc, "tconv_scan_backward");
-        return {packed ? both : gx, packed ? Tensor() : gg, gh0, Tensor(), Tensor()};
+        return {gx, gg, gh0, Tensor(), Tensor()};
     }
 };
 
@@ -251,9 +281,9 @@ std::tuple<Tensor, Tensor> gated_scan(const Tensor& x, const OptTensor& gate_, c
         const variable_list r = GatedScan::apply(x, gate_, h0_, lengths, q8);
         return {r[0], r[1]};
     }
-    at::NoGradGuard off;
-    ScanKept k;
-    return scan_forward(signals(x, gate), h0, given(lengths), false, false, k);
+    at::AutoDispatchBelowADInplaceOrView below;
+    ScanOut o = scan_forward(signals(x, gate), h0, given(lengths), false, false);
+    return {o.y, o.last};
 }
 
 std::tuple<Tensor, Tensor> gated_scan_step(const Tensor& h, const Tensor& x, const OptTensor& gate_, const OptTensor& out_) {
@@ -263,7 +293,7 @@ std::tuple<Tensor, Tensor> gated_scan_step(const Tensor& h, const Tensor& x, con
     TORCH_CHECK_VALUE(x.is_cuda(), "x: need a CUDA tensor, got one on ", x.device());
     TORCH_CHECK_VALUE(x.dim() == 2, "x: need a tensor of 2 dimensions, got ", x.dim());
     c10::cuda::CUDAGuard guard(x.device());
-    at::NoGradGuard off;
+    at::AutoDispatchBelowADInplaceOrView below;
     const Signals s = signals(x.unsqueeze(2), gate.defined() ? gate.unsqueeze(-1) : gate);
     const int64_t nc[2] = {s.d.N, s.d.C};
     same(h, x, at::kFloat, nc, "h");
@@ -278,10 +308,10 @@ std::tuple<Tensor, Tensor> gated_scan_step(const Tensor& h, const Tensor& x, con
         TORCH_CHECK_VALUE(lo(out) == lo(h0) || hi(out) <= lo(h0) || hi(h0) <= lo(out), "out: overlaps h without being it");
         last = out;
     } else {
-        last = at::empty(nc, h0.options());
+        last = fresh(nc, at::kFloat, h0);
     }
-    Tensor y = at::empty(nc, s.x.options());
-    const int rc = tconv_scan_forward(&s.d, ptr(s.x), ptr(s.g), fptr(h0), nullptr, ptr(y), fptr(last), nullptr, nullptr, nullptr,
+    Tensor y = fresh(nc, s.type, s.x);
+    const int rc = tconv_scan_forward(&s.d, s.px, s.pg, fptr(h0), nullptr, ptr(y), fptr(last), nullptr, nullptr, nullptr,
                                       nullptr, nullptr, nullptr, 0, stream());
     if (rc) fail(rc, "tconv_scan_forward");
     if (out.defined()) out.unsafeGetTensorImpl()->bump_version();
@@ -299,16 +329,25 @@ tconv_norm_desc_t norm_desc(const Tensor& x, double eps) {
     return tconv_norm_desc_t{(int32_t)x.size(0), (int32_t)x.size(1), P, dtype_of(x, "x"), (float)eps};
 }
 
+// What a backward pass needs beside the stream: rstd, and where asked for the stream in 8 bits, in one buffer.
 struct NormKept {
-    Tensor s, rstd, w;
-    Q8 q;
+    size_t rstd, codes, scales, size;
+    NormKept(const tconv_norm_desc_t& d, int64_t rows, int64_t inner, bool q8) {
+        Places p;
+        rstd = p.add((size_t)d.N * d.P * sizeof(float));
+        if (q8) {
+            codes = p.add(tconv_q8_codes_bytes(rows, inner));
+            scales = p.add(tconv_q8_scales_bytes(rows, inner));
+        }
+        size = p.end;
+    }
 };
 struct NormOut {
-    Tensor y, sum;
+    Tensor y, sum, stream, w, kept;
     Q8 q;
 };
 
-NormOut norm_forward(const Tensor& x, const Tensor& weight, const Tensor& residual, double eps, int output, bool keep, bool q8, NormKept& k) {
+NormOut norm_forward(const Tensor& x, const Tensor& weight, const Tensor& residual, double eps, int output, bool keep, bool q8) {
     const tconv_norm_desc_t d = norm_desc(x, eps);
     const int64_t c[1] = {d.C};
     TORCH_CHECK_VALUE(weight.device() == x.device() && weight.sizes() == at::IntArrayRef(c), "weight: need a tensor of shape ", at::IntArrayRef(c),
@@ -316,17 +355,19 @@ NormOut norm_forward(const Tensor& x, const Tensor& weight, const Tensor& residu
     same(residual, x, x.scalar_type(), x.sizes(), "residual");
     const auto [rows, inner] = q8_rows(x.sizes());
     const Tensor xc = dense(x), rc_ = dense(residual);
-    k.w = dense(weight.to(at::kFloat));
-    const auto opt = xc.options();
+    const at::ScalarType type = x.scalar_type();
+    const NormKept k(d, rows, inner, q8);
     NormOut o;
-    if (output != kQ8) o.y = at::empty(x.sizes(), opt);
-    if (residual.defined()) o.sum = at::empty(x.sizes(), opt);
+    o.w = dense(weight.scalar_type() == at::kFloat ? weight : weight.to(at::kFloat));
+    if (output != kQ8) o.y = fresh(x.sizes(), type, x);
+    if (residual.defined()) o.sum = fresh(x.sizes(), type, x);
     if (output != kSame) o.q = q8_empty(x, rows, inner);
-    if (keep) k.rstd = at::empty({d.N * d.P}, opt.dtype(at::kFloat));
-    if (keep && q8) k.q = q8_empty(x, rows, inner);
-    if (keep && !q8) k.s = residual.defined() ? o.sum : xc;
-    const int rc = tconv_norm_forward(&d, ptr(xc), ptr(rc_), fptr(k.w), ptr(o.sum), ptr(o.y), fptr(k.rstd), ptr(o.q.codes),
-                                      ptr(o.q.scales), ptr(k.q.codes), ptr(k.q.scales), stream());
+    if (keep) o.kept = bytes(k.size, x);
+    o.stream = residual.defined() ? o.sum : xc;
+    char* b = keep ? (char*)ptr(o.kept) : nullptr;
+    const int rc = tconv_norm_forward(&d, ptr(xc), ptr(rc_), fptr(o.w), ptr(o.sum), ptr(o.y), keep ? (float*)(b + k.rstd) : nullptr,
+                                      ptr(o.q.codes), ptr(o.q.scales), keep && q8 ? b + k.codes : nullptr, keep && q8 ? b + k.scales : nullptr,
+                                      stream());
     if (rc) fail(rc, "tconv_norm_forward");
     return o;
 }
@@ -336,13 +377,13 @@ public:
     // y, then the sum where there is a residual, then codes and scales where y is wanted in 8 bits too
     static variable_list forward(AutogradContext* ctx, const Variable& x, const Variable& weight, const OptTensor& residual_, double eps,
                                  int64_t output, bool q8) {
+        at::AutoDispatchBelowADInplaceOrView below;
         const Tensor residual = given(residual_);
         ctx->set_materialize_grads(false);
-        NormKept k;
-        const NormOut o = norm_forward(x, weight, residual, eps, (int)output, true, q8, k);
-        ctx->saved_data["eps"] = eps;
-        ctx->saved_data["shape"] = x.sizes().vec();
-        ctx->saved_data["how"] = std::vector<int64_t>{x.scalar_type() == at::kFloat ? TCONV_F32 : TCONV_BF16, q8, residual.defined()};
+        const NormOut o = norm_forward(x, weight, residual, eps, (int)output, true, q8);
+        std::vector<int64_t> how{x.scalar_type() == at::kFloat ? TCONV_F32 : TCONV_BF16, q8, residual.defined()};
+        how.insert(how.end(), x.sizes().begin(), x.sizes().end());
+        ctx->saved_data["how"] = how;
         variable_list r{o.y};
         if (o.sum.defined()) r.push_back(o.sum);
         if (o.q.codes.defined()) {
@@ -350,51 +391,47 @@ public:
             r.push_back(o.q.scales);
             ctx->mark_non_differentiable({o.q.codes, o.q.scales});
         }
-        if (q8)
-            ctx->save_for_backward({k.q.codes, k.q.scales, k.rstd, k.w});
-        else
-            ctx->save_for_backward({k.s, k.rstd, k.w});
+        if (q8) ctx->save_for_backward({o.kept, o.w});
+        else ctx->save_for_backward({o.kept, o.w, o.stream});
         return r;
     }
     static variable_list backward(AutogradContext* ctx, variable_list go) {
         once("rms_norm");
         const auto v = ctx->get_saved_variables();
-        const auto shape = ctx->saved_data["shape"].toIntVector();
         const auto how = ctx->saved_data["how"].toIntVector();
+        at::AutoDispatchBelowADInplaceOrView below;
+        const at::IntArrayRef shape(how.data() + 3, how.size() - 3);
         const bool q8 = how[1], res = how[2];
         const Tensor gsum = res ? go[1] : Tensor();
         if (!go[0].defined() && !gsum.defined()) return variable_list(6);
         const at::ScalarType type = how[0] == TCONV_F32 ? at::kFloat : at::kBFloat16;
-        const Tensor rstd = v[q8 ? 2 : 1], w = v[q8 ? 3 : 2];
-        TORCH_CHECK_VALUE(rstd.defined() && rstd.is_cuda(), "rstd: need the CUDA tensor that the forward saved");
-        c10::cuda::CUDAGuard guard(rstd.device());
+        TORCH_CHECK_VALUE(v[0].defined() && v[0].is_cuda() && v[1].defined(), "rstd, weight: need the CUDA tensors that the forward saved");
+        c10::cuda::CUDAGuard guard(v[0].device());
         const auto [rows, inner] = q8_rows(shape);
         int64_t P = 1;
         for (size_t i = 2; i < shape.size(); ++i) P *= shape[i];
-        const tconv_norm_desc_t d{(int32_t)shape[0], (int32_t)shape[1], P, (int32_t)how[0], (float)ctx->saved_data["eps"].toDouble()};
-        const int64_t np[1] = {shape[0] * P}, c[1] = {shape[1]};
-        same(rstd, rstd, at::kFloat, np, "rstd");
-        same(w, rstd, at::kFloat, c, "weight");
+        const tconv_norm_desc_t d{(int32_t)shape[0], (int32_t)shape[1], P, (int32_t)how[0], 0.0f};
+        const NormKept k(d, rows, inner, q8);
+        const int64_t size[1] = {(int64_t)k.size}, c[1] = {shape[1]};
+        same(v[0], v[0], at::kByte, size, "rstd");
+        same(v[1], v[0], at::kFloat, c, "weight");
         Tensor s;
-        Q8 q;
-        if (q8) {
-            q = {v[0], v[1]};
-            q8_check(q, rstd, rows, inner);
-        } else {
-            TORCH_CHECK_VALUE(v[0].defined(), "s: need the tensor that the forward saved");
-            same(v[0], rstd, type, shape, "s");
-            s = dense(v[0]);
+        if (!q8) {
+            TORCH_CHECK_VALUE(v[2].defined(), "s: need the tensor that the forward saved");
+            same(v[2], v[0], type, shape, "s");
+            s = dense(v[2]);
         }
-        same(go[0], rstd, type, shape, "grad_y");
-        same(gsum, rstd, type, shape, "grad_sum");
-        const auto opt = rstd.options().dtype(type);
-        const Tensor gy = go[0].defined() ? dense(go[0]) : at::zeros(shape, opt), gs = dense(gsum), rs = dense(rstd), wc = dense(w);
-        Tensor gx = at::empty(shape, opt), gw, ws;
-        if (ctx->needs_input_grad(1)) gw = at::empty(c, opt.dtype(at::kFloat));
-        const size_t n = tconv_norm_workspace_bytes(&d);
-        if (n) ws = at::empty({(int64_t)n}, opt.dtype(at::kByte));
-        const int rc = tconv_norm_backward(&d, ptr(s), ptr(q.codes), ptr(q.scales), fptr(rs), fptr(wc), ptr(gy), ptr(gs), ptr(gx), fptr(gw),
-                                           ptr(ws), n, stream());
+        same(go[0], v[0], type, shape, "grad_y");
+        same(gsum, v[0], type, shape, "grad_sum");
+        const Tensor kept = dense(v[0]), w = dense(v[1]), gs = dense(gsum);
+        const Tensor gy = go[0].defined() ? dense(go[0]) : at::zeros(shape, kept.options().dtype(type));
+        Tensor gx = fresh(shape, type, kept), gw;
+        if (ctx->needs_input_grad(1)) gw = fresh(c, at::kFloat, kept);
+        const size_t n = gw.defined() ? tconv_norm_workspace_bytes(&d) : 0;
+        const Tensor ws = bytes(n, kept);
+        const char* b = (const char*)ptr(kept);
+        const int rc = tconv_norm_backward(&d, ptr(s), q8 ? b + k.codes : nullptr, q8 ? b + k.scales : nullptr, (const float*)(b + k.rstd),
+                                           fptr(w), ptr(gy), ptr(gs), ptr(gx), fptr(gw), ptr(ws), n, stream());
         if (rc) fail(rc, "tconv_norm_backward");
         return {gx, gw, res ? gx : Tensor(), Tensor(), Tensor(), Tensor()};
     }
@@ -415,9 +452,8 @@ std::tuple<OptTensor, OptTensor, OptTensor, OptTensor> rms_norm(const Tensor& x,
         return {opt(r[0]), residual.defined() ? opt(r[1]) : OptTensor(), output == kBoth ? opt(r[at]) : OptTensor(),
                 output == kBoth ? opt(r[at + 1]) : OptTensor()};
     }
-    at::NoGradGuard off;
-    NormKept k;
-    const NormOut o = norm_forward(x, weight, residual, eps, (int)output, false, false, k);
+    at::AutoDispatchBelowADInplaceOrView below;
+    const NormOut o = norm_forward(x, weight, residual, eps, (int)output, false, false);
     return {opt(o.y), opt(o.sum), opt(o.q.codes), opt(o.q.scales)};
 }
 

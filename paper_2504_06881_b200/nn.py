@@ -556,11 +556,13 @@ class Q8(NamedTuple):
         return self.codes.nbytes + self.scales.nbytes
 
 
+_Q8_TYPES = {t: tconv.DTYPES[name] for name, t in tconv.TORCH_DTYPE.items()}
+
+
 def _q8_type(dtype):
-    for name, t in tconv.TORCH_DTYPE.items():
-        if t == dtype:
-            return tconv.DTYPES[name]
-    raise ValueError(f"dtype: need float32 or bfloat16, got {dtype}")
+    if dtype not in _Q8_TYPES:
+        raise ValueError(f"dtype: need float32 or bfloat16, got {dtype}")
+    return _Q8_TYPES[dtype]
 
 
 def _kept(checkpoint):
@@ -572,7 +574,7 @@ def _kept(checkpoint):
 def q8_store(x) -> Q8:
     """x (float32 or bfloat16, on the GPU) in 8 bits; no gradients."""
     codes, scales = _native.q8_store(x)
-    return Q8(codes, scales, tuple(x.shape), x.dtype)
+    return Q8(codes, scales, x.shape, x.dtype)
 
 
 def gated_scan(x, gate=None, h0=None, lengths=None, checkpoint=None):
@@ -610,7 +612,7 @@ def rms_norm(x, weight, residual=None, eps=1e-6, output="same", checkpoint=None)
     if output not in _OUTPUTS:
         raise ValueError(f"output must be one of {tuple(_OUTPUTS)}, got {output!r}")
     y, s, codes, scales = _native.rms_norm(x, weight, residual, eps, _OUTPUTS[output], _kept(checkpoint))
-    return NormOutput(y, x if s is None else s, None if codes is None else Q8(codes, scales, tuple(x.shape), x.dtype))
+    return NormOutput(y, x if s is None else s, None if codes is None else Q8(codes, scales, x.shape, x.dtype))
 
 
 class RMSNorm(nn.Module):
