@@ -280,29 +280,46 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
     float gw[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) gw[j] = 0.0f;
-    for (uint32_t tile = blockIdx.x; tile < all; tile += gridDim.x) {
-        const uint32_t n = tile / tiles, p0 = (tile - n * tiles) * kQ8Block, p = p0 + b.lp * V;
-        const int live = p < P ? have : 0;
-        const int64_t image = (int64_t)n * a.C * P, row0 = (int64_t)n * a.C + b.c0;
-        const uint32_t at = b.c0 * P + p;
-        const T *ps = (const T*)k.s + image, *py = (const T*)k.gy + image, *pg = (const T*)k.gs + image;
-        Kept<T, V, Q8> s[R];
-        Some<T, V> dy[R], ds[RES ? (kLate ? kBatch : R) : 1];
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            s[j].none();
-            dy[j] = none_of<T, V>();
-            if (j < live) {
-                const int64_t row = row0 + j * b.kStep;
-                s[j].load(ps + (at + j * step), k.sc + row * pitch + p, k.ss + row * tiles + p0 / kQ8Block);
-                dy[j] = load_some<T, V>(py, at + j * step);
-            }
+    // A tile's place.  The registers of a channel take the next tile's values as soon as this one's are done with, so that the
+    // reads go on while the rest is written and summed.
+    struct At {
+        uint32_t n, p0, p, in_image;
+        int live;
+    };
+    const auto place = [&](uint32_t tile) {
+        At t;
+        t.n = tile / tiles;
+        t.p0 = (tile - t.n * tiles) * kQ8Block;
+        t.p = t.p0 + b.lp * V;
+        t.in_image = b.c0 * P + t.p;
+        t.live = tile < all && t.p < P ? have : 0;
+        return t;
+    };
+    Kept<T, V, Q8> s[R];
+    Some<T, V> dy[R], ds[RES ? (kLate ? kBatch : R) : 1];
+    const auto load = [&](const At& t, int j) {
+        s[j].none();
+        dy[j] = none_of<T, V>();
+        if constexpr (RES && !kLate) ds[j] = none_of<T, V>();
+        if (j < t.live) {
+            const int64_t image = (int64_t)t.n * a.C * P, row = (int64_t)t.n * a.C + b.c0 + j * b.kStep;
+            const uint32_t at = t.in_image + j * step;
+            s[j].load((const T*)k.s + image + at, k.sc + row * pitch + t.p, k.ss + row * tiles + t.p0 / kQ8Block);
+            dy[j] = load_some<T, V>((const T*)k.gy + image, at);
+            if constexpr (RES && !kLate) ds[j] = load_some<T, V>((const T*)k.gs + image, at);
         }
+    };
+    At t = place(blockIdx.x);
+#pragma unroll
+    for (int j = 0; j < R; ++j) load(t, j);
+    for (uint32_t tile = blockIdx.x; tile < all; tile += gridDim.x) {
+        const At next = place(tile + gridDim.x);
+        const int64_t image = (int64_t)t.n * a.C * P;
         float rstd[V], m[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) rstd[i] = m[i] = 0.0f;
-        if (p < P) {
-            const float* pr = k.rstd + (int64_t)n * P + p;
+        if (t.p < P) {
+            const float* pr = k.rstd + (int64_t)t.n * P + t.p;
             if constexpr (V == 1) rstd[0] = __ldg(pr);
             else
 #pragma unroll
@@ -310,13 +327,6 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
                     const float4 q = __ldg(reinterpret_cast<const float4*>(pr + i));
                     rstd[i] = q.x; rstd[i + 1] = q.y; rstd[i + 2] = q.z; rstd[i + 3] = q.w;
                 }
-        }
-        if constexpr (RES && !kLate) {
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                ds[j] = none_of<T, V>();
-                if (j < live) ds[j] = load_some<T, V>(pg, at + j * step);
-            }
         }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -326,12 +336,12 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
             spread<T, V>(dy[j], d);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float t = d[i] * (v[i] * rstd[i]);
-                gw[j] += t;
-                m[i] = fmaf(wc, t, m[i]);
+                const float u = d[i] * (v[i] * rstd[i]);
+                gw[j] += u;
+                m[i] = fmaf(wc, u, m[i]);
             }
         }
-        b.sum(m, part, total, [&](float t, int) { return t / (float)a.C; });
+        b.sum(m, part, total, [&](float u, int) { return u / (float)a.C; });
         T* po = gx + image;
 #pragma unroll
         for (int j0 = 0; j0 < R; j0 += kBatch) {
@@ -339,7 +349,7 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
                     ds[j] = none_of<T, V>();
-                    if (j0 + j < live) ds[j] = load_some<T, V>(pg, at + (j0 + j) * step);
+                    if (j0 + j < t.live) ds[j] = load_some<T, V>((const T*)k.gs + image, t.in_image + (j0 + j) * step);
                 }
             }
 #pragma unroll
@@ -357,9 +367,14 @@ __global__ void __launch_bounds__(WARPS * 32, norm_resident(WARPS)) norm_bwd_col
 #pragma unroll
                     for (int i = 0; i < V; ++i) d[i] += e[i];
                 }
-                if (j < live) store_some<T, V>(po, at + j * step, gather<T, V>(d));
+                if (j < t.live) store_some<T, V>(po, t.in_image + j * step, gather<T, V>(d));
+                if constexpr (!kLate) load(next, j);
             }
         }
+        if constexpr (kLate)                                  // (no registers to spare for reads on their way)
+#pragma unroll
+            for (int j = 0; j < R; ++j) load(next, j);
+        t = next;
     }
     if (!gw_part) return;
 #pragma unroll

@@ -142,59 +142,86 @@ __global__ void __launch_bounds__(256) q8_store_kernel(int64_t rows, int64_t inn
     }
 }
 
-// ROWS: rows are whole vectors, a thread restores 8 values of one; else it restores 8 values that lie next to each other in the
-// result, whose writes are the ones that have to be whole, from wherever their codes are.
-template <typename T, typename I, bool ROWS>
+// Eight values that lie next to each other.  fp32: as 32 bytes where x starts on 32 (two stores of 16 would each reach half of every
+// sector).
+template <typename T> __device__ __forceinline__ void write_eight(T* x, const float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        if ((reinterpret_cast<uintptr_t>(x) & 31) == 0) {
+            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(x), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                         "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) reinterpret_cast<float4*>(x)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&p);
+        }
+        *reinterpret_cast<uint4*>(x) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// Rows of whole units of eight: a thread restores kRestore units, 256 apart (one read of 8 bytes a thread would leave the memory
+// waiting: 42 us with one unit, 38 with two, for 67 million bf16 values).
+constexpr int kRestore = 2;
+template <typename T, typename I>
 __global__ void __launch_bounds__(256) q8_restore_kernel(int64_t rows, int64_t inner, const int8_t* __restrict__ codes,
                                                          const uint8_t* __restrict__ scales, T* __restrict__ x) {
-    constexpr int kWords = sizeof(T) / 2;
+    const I nb = (I)q8_blocks(inner), units = (I)(rows * inner / 8), per_row = (I)(inner / 8);
+    const I first = (I)blockIdx.x * (256 * kRestore) + threadIdx.x;
+    uint2 c[kRestore];
+    uint32_t byte[kRestore];
+#pragma unroll
+    for (int j = 0; j < kRestore; ++j) {
+        const I u = first + 256 * j;
+        if (u >= units) continue;
+        const I row = u / per_row, at = u - row * per_row;
+        c[j] = __ldg(reinterpret_cast<const uint2*>(codes) + u);
+        byte[j] = __ldg(scales + (int64_t)row * nb + at / (kQ8Block / 8));
+    }
+#pragma unroll
+    for (int j = 0; j < kRestore; ++j) {
+        const I u = first + 256 * j;
+        if (u >= units) continue;
+        float v[8];
+        decode_eight(c[j], byte[j], v);
+        write_eight(x + (int64_t)u * 8, v);
+    }
+}
+
+// Other rows: a thread restores eight values that lie next to each other in the result, whose writes are the ones that have to be
+// whole, from wherever their codes are.
+template <typename T, typename I>
+__global__ void __launch_bounds__(256) q8_restore_any_kernel(int64_t rows, int64_t inner, const int8_t* __restrict__ codes,
+                                                             const uint8_t* __restrict__ scales, T* __restrict__ x) {
     const I nb = (I)q8_blocks(inner), total = (I)(rows * inner);
     const int64_t pitch = q8_pitch(inner);
     const I first = ((I)blockIdx.x * 256 + threadIdx.x) * 8;
     if (first >= total) return;
     I row = first / (I)inner, at = first - row * (I)inner;
     float v[8];
-    if constexpr (ROWS) {
-        const uint2 c = __ldg(reinterpret_cast<const uint2*>(codes + (int64_t)row * pitch + at));
-        decode_eight(c, __ldg(scales + (int64_t)row * nb + at / kQ8Block), v);
-    } else {
-        int q[8];
-        uint32_t b[8];
+    int q[8];
+    uint32_t b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            q[i] = 0;
-            b[i] = 1;
-            if (first + i < total) {
-                q[i] = __ldg(codes + (int64_t)row * pitch + at);
-                b[i] = __ldg(scales + (int64_t)row * nb + at / kQ8Block);
-            }
-            if (++at == (I)inner) { at = 0; ++row; }
+    for (int i = 0; i < 8; ++i) {
+        q[i] = 0;
+        b[i] = 1;
+        if (first + i < total) {
+            q[i] = __ldg(codes + (int64_t)row * pitch + at);
+            b[i] = __ldg(scales + (int64_t)row * nb + at / kQ8Block);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)q[i] * q8_unit(b[i]);
+        if (++at == (I)inner) { at = 0; ++row; }
     }
-    if (sizeof(T) == 4 && first + 8 <= total && (reinterpret_cast<uintptr_t>(x) & 31) == 0) {
-        // (two stores of 16 bytes would each reach half of every sector)
-        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(x + first), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
-                     "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
-    } else if (first + 8 <= total) {
-        uint32_t w[4 * kWords];
 #pragma unroll
-        for (int i = 0; i < 4 * kWords; ++i) {
-            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
-            else {
-                const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&p);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kWords; ++j)
-            reinterpret_cast<uint4*>(x + first)[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-    } else {
+    for (int i = 0; i < 8; ++i) v[i] = (float)q[i] * q8_unit(b[i]);
+    if (first + 8 <= total) write_eight(x + first, v);
+    else
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (first + i < total) x[first + i] = from_f32<T>(v[i]);
-    }
 }
 
 }  // namespace tconv

@@ -30,9 +30,12 @@ template <typename T, typename I> int q8_store_t(Q8Rows q, const void* x, void* 
     return launched(1, "q8_store");
 }
 template <typename T, typename I> int q8_restore_t(Q8Rows q, const void* codes, const void* scales, void* x, cudaStream_t st) {
-    const unsigned grid = (unsigned)(((q.rows * q.inner + 7) / 8 + 255) / 256);
-    const auto kern = q.inner % 8 == 0 ? q8_restore_kernel<T, I, true> : q8_restore_kernel<T, I, false>;
-    kern<<<grid, 256, 0, st>>>(q.rows, q.inner, (const int8_t*)codes, (const uint8_t*)scales, (T*)x);
+    const int64_t units = (q.rows * q.inner + 7) / 8;
+    if (q.inner % 8 == 0)
+        q8_restore_kernel<T, I><<<(unsigned)((units + 256 * kRestore - 1) / (256 * kRestore)), 256, 0, st>>>(q.rows, q.inner, (const int8_t*)codes,
+                                                                                                             (const uint8_t*)scales, (T*)x);
+    else
+        q8_restore_any_kernel<T, I><<<(unsigned)((units + 255) / 256), 256, 0, st>>>(q.rows, q.inner, (const int8_t*)codes, (const uint8_t*)scales, (T*)x);
     return launched(1, "q8_restore");
 }
 template <typename F> int q8_types(Q8Rows q, int dtype, F f) {
