@@ -234,7 +234,8 @@ public:
     // (missing tensors as empty optionals: an undefined tensor argument is not a variable to the engine)
     static Variable forward(AutogradContext* ctx, const Variable& x, const Variable& w, const std::optional<Variable>& w2_,
                             const std::optional<Variable>& alpha_, const std::optional<Variable>& beta_,
-                            const std::optional<Variable>& bias_, const Geom& g) {
+                            const std::optional<Variable>& bias_, const Geom& g, bool q8, const std::optional<Variable>& codes_,
+                            const std::optional<Variable>& scales_) {
         const Tensor w2 = given(w2_), alpha = given(alpha_), beta = given(beta_), bias = given(bias_);
         Saved s;
         Tensor y = run_forward(g, x, w, w2, alpha, beta, bias, true, s);
@@ -243,28 +244,52 @@ public:
                                                        g.pad[0], g.pad[1], g.pad[2], g.dil[0], g.dil[1], g.dil[2]};
         ctx->saved_data["given"] = (int64_t)((w2.defined() ? 1 : 0) | (alpha.defined() ? 2 : 0) | (beta.defined() ? 4 : 0) |
                                              (bias.defined() ? 8 : 0));
-        ctx->save_for_backward({s.x, s.w, s.w2, s.alpha, s.beta, s.winners});
+        if (q8) {       // x in 8 bits, as the caller has it or stored here
+            const auto [rows, inner] = tconv_torch::q8_rows(x.sizes());
+            c10::cuda::CUDAGuard guard(x.device());
+            tconv_torch::Q8 q{given(codes_), given(scales_)};
+            if (q.codes.defined()) {
+                tconv_torch::q8_check(q, x, rows, inner);
+            } else {
+                q = tconv_torch::q8_empty(x, rows, inner);
+                if (const int rc = tconv_q8_store(rows, inner, g.dtype, ptr(s.x), ptr(q.codes), ptr(q.scales), stream())) fail(rc, "tconv_q8_store");
+            }
+            ctx->saved_data["x"] = x.sizes().vec();
+            ctx->save_for_backward({q.codes, s.w, s.w2, s.alpha, s.beta, s.winners, q.scales});
+        } else {
+            ctx->save_for_backward({s.x, s.w, s.w2, s.alpha, s.beta, s.winners});
+        }
         return y.scalar_type() == x.scalar_type() ? y : y.to(x.scalar_type());
     }
     static variable_list backward(AutogradContext* ctx, variable_list gys) {
         const auto v = ctx->get_saved_variables();
-        const Saved s{v[0], v[1], v[2], v[3], v[4], v[5]};
+        Saved s{v[0], v[1], v[2], v[3], v[4], v[5]};
         const auto q = ctx->saved_data["geom"].toIntVector();
         const auto n = [&](int i) { return (int)q[i]; };
         const Geom g{n(0), n(1), n(2), n(3), {n(4), n(5), n(6)}, {n(7), n(8), n(9)}, {n(10), n(11), n(12)}};
         const int64_t has = ctx->saved_data["given"].toInt();
-        if (!gys[0].defined()) return variable_list(7);
+        if (!gys[0].defined()) return variable_list(10);
+        if (v.size() == 7) {
+            const auto shape = ctx->saved_data["x"].toIntVector();
+            const auto [rows, inner] = tconv_torch::q8_rows(shape);
+            TORCH_CHECK_VALUE(v[0].defined() && v[0].is_cuda() && v[6].defined(), "codes, scales: need the CUDA tensors that the forward saved");
+            tconv_torch::q8_check({v[0], v[6]}, v[0], rows, inner);
+            c10::cuda::CUDAGuard guard(v[0].device());
+            s.x = at::empty(shape, v[0].options().dtype(type_of(g)));
+            if (const int rc = tconv_q8_restore(rows, inner, g.dtype, ptr(v[0]), ptr(v[6]), ptr(s.x), stream())) fail(rc, "tconv_q8_restore");
+        }
         Grads r = run_backward(g, s, gys[0], ctx->needs_input_grad(0));
         const auto in_type = (at::ScalarType)ctx->saved_data["in_type"].toInt();
         if (r.x.defined() && r.x.scalar_type() != in_type) r.x = r.x.to(in_type);
         const auto if_given = [&](const Tensor& t, int bit) { return (has & bit) ? t : Tensor(); };
-        return {r.x, r.w, if_given(r.w2, 1), if_given(r.alpha, 2), if_given(r.beta, 4), if_given(r.bias, 8), Tensor()};
+        return {r.x, r.w, if_given(r.w2, 1), if_given(r.alpha, 2), if_given(r.beta, 4), if_given(r.bias, 8), Tensor(), Tensor(), Tensor(), Tensor()};
     }
 };
 
 // Nothing while a trace is recorded: the tracer would see the allocations alone.
 std::optional<Tensor> layer(const Geom& g, const Tensor& x, const Tensor& w, const std::optional<Tensor>& w2_, const std::optional<Tensor>& alpha_,
-             const std::optional<Tensor>& beta_, const std::optional<Tensor>& bias_) {
+             const std::optional<Tensor>& beta_, const std::optional<Tensor>& bias_, bool q8, const std::optional<Tensor>& codes,
+             const std::optional<Tensor>& scales) {
     if (at::tracer::impl::is_dispatch_enabled()) return std::nullopt;
     const Tensor w2 = given(w2_), alpha = given(alpha_), beta = given(beta_), bias = given(bias_);
     // (a tangent would be dropped without a word where nothing is recorded)
@@ -273,7 +298,7 @@ std::optional<Tensor> layer(const Geom& g, const Tensor& x, const Tensor& w, con
     bool record = false;
     if (at::GradMode::is_enabled())
         for (const Tensor* t : {&x, &w, &w2, &alpha, &beta, &bias}) record = record || (t->defined() && t->requires_grad());
-    if (record) return TropicalLayer::apply(x, w, w2_, alpha_, beta_, bias_, g);
+    if (record) return TropicalLayer::apply(x, w, w2_, alpha_, beta_, bias_, g, q8, codes, scales);
     Saved s;     // without recording the winner-free kernels run
     Tensor y = run_forward(g, x, w, w2, alpha, beta, bias, false, s);
     return y.scalar_type() == x.scalar_type() ? y : y.to(x.scalar_type());
@@ -291,6 +316,8 @@ PYBIND11_MODULE(_tconv_torch, m) {
         return g;
     }));
     m.def("set_error", [](pybind11::object e) { g_error = e.release().ptr(); });
-    m.def("layer", &layer, pybind11::call_guard<pybind11::gil_scoped_release>());
+    namespace py = pybind11;
+    m.def("layer", &layer, py::arg("geom"), py::arg("x"), py::arg("w"), py::arg("w2"), py::arg("alpha"), py::arg("beta"), py::arg("bias"),
+          py::arg("q8") = false, py::arg("codes") = py::none(), py::arg("scales") = py::none(), py::call_guard<py::gil_scoped_release>());
     tconv_torch::bind_seq(m);
 }

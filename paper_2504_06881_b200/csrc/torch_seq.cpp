@@ -79,11 +79,10 @@ bool records(std::initializer_list<const Tensor*> ts) {
     return false;
 }
 
+}  // namespace
+
 // ---- activations in 8 bits ------------------------------------------------------------------------------------
-struct Q8 {
-    Tensor codes, scales;
-};
-std::pair<int64_t, int64_t> q8_rows(at::IntArrayRef shape) {
+std::pair<int64_t, int64_t> tconv_torch::q8_rows(at::IntArrayRef shape) {
     TORCH_CHECK_VALUE(!shape.empty(), "x: need a tensor of one dimension at least");
     int64_t inner = 1, rows = 1;
     for (size_t i = 2; i < shape.size(); ++i) inner *= shape[i];
@@ -92,17 +91,24 @@ std::pair<int64_t, int64_t> q8_rows(at::IntArrayRef shape) {
     rows = shape[0];
     return {rows, inner == 1 ? shape[1] : 0};
 }
-Q8 q8_empty(const Tensor& like, int64_t rows, int64_t inner) {
+tconv_torch::Q8 tconv_torch::q8_empty(const Tensor& like, int64_t rows, int64_t inner) {
     const int64_t pitch = (inner + 7) / 8 * 8, nb = (inner + 31) / 32;
     const int64_t c[2] = {rows, pitch}, b[2] = {rows, nb};
     return {fresh(c, at::kChar, like), fresh(b, at::kByte, like)};
 }
-void q8_check(const Q8& q, const Tensor& like, int64_t rows, int64_t inner) {
+void tconv_torch::q8_check(const Q8& q, const Tensor& like, int64_t rows, int64_t inner) {
     const int64_t c[2] = {rows, (inner + 7) / 8 * 8}, s[2] = {rows, (inner + 31) / 32};
     same(q.codes, like, at::kChar, c, "codes");
     same(q.scales, like, at::kByte, s, "scales");
     TORCH_CHECK_VALUE(q.codes.is_cuda() && q.codes.is_contiguous() && q.scales.is_contiguous(), "codes, scales: need contiguous CUDA tensors");
 }
+
+namespace {
+
+using tconv_torch::Q8;
+using tconv_torch::q8_check;
+using tconv_torch::q8_empty;
+using tconv_torch::q8_rows;
 
 std::tuple<Tensor, Tensor> q8_store(const Tensor& x) {
     no_trace("q8_store");

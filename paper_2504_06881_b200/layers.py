@@ -55,4 +55,7 @@ for _mode in ("compound", "parallel"):
                                   base=TropicalConv3d)
         __all__.append(_name)
 
-__all__ += ["TropicalDepthwiseConv2d", "TropicalConv1d", "TropicalConv3d"]
+from .nn import RMSNorm, TropicalRecurrent1d, TropicalRecurrentBlock1d  # noqa: E402  (layers over long signals)
+
+__all__ += ["TropicalDepthwiseConv2d", "TropicalConv1d", "TropicalConv3d", "RMSNorm", "TropicalRecurrent1d",
+            "TropicalRecurrentBlock1d"]

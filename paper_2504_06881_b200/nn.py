@@ -46,7 +46,7 @@ _geoms = tconv.KeptPlans(lambda kind, mode, chan, dtype, stride, pad, dil: _nati
     _KINDS[kind], tconv.MODES[mode], tconv.CHANS[chan], tconv.DTYPES[dtype], stride, pad, dil))
 
 
-def _layer(kind, mode, chan, dtype, stride, pad, dil, x, w, w2, alpha, beta, bias):
+def _layer(kind, mode, chan, dtype, stride, pad, dil, x, w, w2, alpha, beta, bias, checkpoint=None, stored=None):
     """One layer through the native autograd path (csrc/torch_layers.cpp).  Under ``torch.jit.trace`` through the
     Python Function, which a trace records as one operation: of the native path it would record the allocations."""
     geom = (kind, mode, chan, dtype, stride, pad, dil)
@@ -56,9 +56,18 @@ def _layer(kind, mode, chan, dtype, stride, pad, dil, x, w, w2, alpha, beta, bia
         stride, pad, dil = tuple(stride), tuple(pad), tuple(dil)
         geom = (kind, mode, chan, dtype, stride, pad, dil)
         g = _geoms.get(geom, *geom)
-    y = _native.layer(g, x, w, w2, alpha, beta, bias)
+    if checkpoint is None:
+        if stored is not None:
+            raise ValueError("stored: only a layer with checkpoint='q8' takes its input's 8-bit form")
+        y = _native.layer(g, x, w, w2, alpha, beta, bias)
+    elif stored is None:
+        y = _native.layer(g, x, w, w2, alpha, beta, bias, True)
+    else:
+        y = _native.layer(g, x, w, w2, alpha, beta, bias, True, stored.codes, stored.scales)
     if y is not None:
         return y
+    if checkpoint is not None:
+        raise NotImplementedError("a layer with checkpoint='q8' cannot be traced")
     fn = {"dense": TropicalConvFn, "depthwise": TropicalDepthwiseFn, "volume": TropicalConv3dFn}[kind]
     return fn.apply(x, w, w2, alpha, beta, bias, (mode, dtype, stride, pad, dil) if kind == "depthwise" else geom[1:])
 
@@ -243,7 +252,7 @@ class TropicalConvBNFn(torch.autograd.Function):
 def tropical_conv_bn(conv: "TropicalConv2d", bn: nn.BatchNorm2d, x):
     """conv followed by bn; in training mode with the layer's fused channel statistics."""
     if not (bn.training and x.is_cuda and conv.bias is None and bn.affine and bn.track_running_stats
-            and conv.params in ("2p", "0p") and type(conv) is TropicalConv2d):
+            and conv.params in ("2p", "0p") and conv.checkpoint is None and type(conv) is TropicalConv2d):
         return bn(conv(x))
     geom = (conv.mode, conv.chan, conv.dtype, conv.stride, conv.padding, conv.dilation)
     out, mean, var = TropicalConvBNFn.apply(x, conv.weight, conv.weight2, conv.alpha, conv.beta, bn.weight, bn.bias,
@@ -265,15 +274,21 @@ class TropicalConv2d(nn.Module):
     per (c_out, c_in); "1p" complementary weights beta = 1 - alpha; "shared" beta = alpha;
     "opposite" beta = -alpha; "0p" alpha = beta = 1 (no scalars); "fixed" the constants
     ``fixed=(alpha, beta)``, e.g. (0.5, 0.5) or (1, -1), held as buffers.
-    dtype: arithmetic type of the kernels ("f32" or "bf16"); parameters stay fp32."""
+    dtype: arithmetic type of the kernels ("f32" or "bf16"); parameters stay fp32.
+    checkpoint="q8": the backward pass keeps the input in 8 bits (see Q8) in place of the tensor itself.  It is read for
+    the gradients of alpha and beta alone, which are then those over the restored input; all others are the same.
+    forward's `stored` is the input's Q8 where it is there already (rms_norm's second output)."""
 
     PARAMS = ("0p", "1p", "2p", "shared", "opposite", "fixed")
     ND = 2          # spatial dimensions
     KIND = "dense"
+    checkpoint = None
 
     def __init__(self, in_channels, out_channels, kernel_size, stride=1, padding=0, dilation=1,
-                 bias=True, mode="compound", chan="default", params="2p", dtype="f32", fixed=(0.5, 0.5)):
+                 bias=True, mode="compound", chan="default", params="2p", dtype="f32", fixed=(0.5, 0.5), checkpoint=None):
         super().__init__()
+        _kept(checkpoint)
+        self.checkpoint = checkpoint
         two = lambda v: (v,) * self.ND if isinstance(v, int) else tuple(v)
         self.kernel_size, self.stride, self.padding, self.dilation = map(two, (kernel_size, stride, padding, dilation))
         self.in_channels, self.out_channels = in_channels, out_channels
@@ -307,9 +322,9 @@ class TropicalConv2d(nn.Module):
     def extra_repr(self):
         return (f"{self.in_channels}, {self.out_channels}, kernel_size={self.kernel_size}, stride={self.stride}, "
                 f"padding={self.padding}, dilation={self.dilation}, mode={self.mode}, chan={self.chan}, "
-                f"params={self.params}, dtype={self.dtype}")
+                f"params={self.params}, dtype={self.dtype}" + (f", checkpoint={self.checkpoint}" if self.checkpoint else ""))
 
-    def forward(self, x):
+    def forward(self, x, stored=None):
         alpha, beta = self.alpha, self.beta
         if self.mode in ("compound", "parallel"):
             if self.params == "1p":
@@ -321,10 +336,12 @@ class TropicalConv2d(nn.Module):
             elif self.params == "fixed":
                 alpha, beta = self.alpha_fixed, self.beta_fixed
         if self.KIND == "dense" and (TropicalConvFn.events is not None or TropicalConvFn.fuse_cast):
+            if self.checkpoint is not None:
+                raise ValueError("checkpoint='q8' goes with neither TropicalConvFn.events nor TropicalConvFn.fuse_cast")
             geom = (self.mode, self.chan, self.dtype, self.stride, self.padding, self.dilation, torch.is_grad_enabled())
             return TropicalConvFn.apply(x, self.weight, self.weight2, alpha, beta, self.bias, geom)
         return _layer(self.KIND, self.mode, self.chan, self.dtype, self.stride, self.padding, self.dilation, x,
-                      self.weight, self.weight2, alpha, beta, self.bias)
+                      self.weight, self.weight2, alpha, beta, self.bias, self.checkpoint, stored)
 
 
 class TropicalBasicBlock(nn.Module):
@@ -419,11 +436,15 @@ class TropicalDepthwiseConv2d(nn.Module):
     """Depthwise tropical convolution (``nn.Conv2d(channels, channels, k, groups=channels)``'s place in
     a MobileNetV2 block): per channel one window of weights, one alpha and one beta.
 
-    mode and params as in TropicalConv2d ("2p", "1p", "shared", "opposite", "0p", "fixed")."""
+    mode, params and checkpoint as in TropicalConv2d ("2p", "1p", "shared", "opposite", "0p", "fixed")."""
+
+    checkpoint = None
 
     def __init__(self, channels, kernel_size, stride=1, padding=0, dilation=1, bias=True,
-                 mode="compound", params="2p", dtype="f32", fixed=(0.5, 0.5)):
+                 mode="compound", params="2p", dtype="f32", fixed=(0.5, 0.5), checkpoint=None):
         super().__init__()
+        _kept(checkpoint)
+        self.checkpoint = checkpoint
         two = lambda v: (v, v) if isinstance(v, int) else tuple(v)
         self.kernel_size, self.stride, self.padding, self.dilation = map(two, (kernel_size, stride, padding, dilation))
         self.channels, self.mode, self.params, self.dtype = channels, mode, params, dtype
@@ -449,9 +470,10 @@ class TropicalDepthwiseConv2d(nn.Module):
 
     def extra_repr(self):
         return (f"{self.channels}, kernel_size={self.kernel_size}, stride={self.stride}, padding={self.padding}, "
-                f"dilation={self.dilation}, mode={self.mode}, params={self.params}, dtype={self.dtype}")
+                f"dilation={self.dilation}, mode={self.mode}, params={self.params}, dtype={self.dtype}" +
+                (f", checkpoint={self.checkpoint}" if self.checkpoint else ""))
 
-    def forward(self, x):
+    def forward(self, x, stored=None):
         alpha, beta = self.alpha, self.beta
         if self.mode in ("compound", "parallel"):
             if self.params == "1p":
@@ -463,7 +485,7 @@ class TropicalDepthwiseConv2d(nn.Module):
             elif self.params == "fixed":
                 alpha, beta = self.alpha_fixed, self.beta_fixed
         return _layer("depthwise", self.mode, "sum", self.dtype, self.stride, self.padding, self.dilation, x, self.weight,
-                      self.weight2, alpha, beta, self.bias)
+                      self.weight2, alpha, beta, self.bias, self.checkpoint, stored)
 
 
 class TropicalConv3dFn(torch.autograd.Function):
@@ -509,31 +531,31 @@ class TropicalConv3d(TropicalConv2d):
 
 class TropicalConv1d(nn.Module):
     """1-D tropical convolution (Section 3.2) with ``nn.Conv1d``'s constructor arguments; mode / chan /
-    params / dtype as in TropicalConv2d.  The length-3, stride-1 layers run as 1 x 3 windows on a signal
+    params / dtype / checkpoint as in TropicalConv2d.  The length-3, stride-1 layers run as 1 x 3 windows on a signal
     of unit height through the tiled 2-D kernels; every other window (up to 256 taps; the paper's audio
     networks open with length 80 at stride 4) goes as a 1 x 1 x k window through the three-dimensional
     entry points, which run windows of four taps or more at stride 1, 2 or 4 (no dilation) on their
     one-dimensional kernels and the rest on the any-shape kernels."""
 
     def __init__(self, in_channels, out_channels, kernel_size, stride=1, padding=0, dilation=1,
-                 bias=True, mode="compound", chan="default", params="2p", dtype="f32", fixed=(0.5, 0.5)):
+                 bias=True, mode="compound", chan="default", params="2p", dtype="f32", fixed=(0.5, 0.5), checkpoint=None):
         super().__init__()
         self.tiled = (kernel_size == 3 and stride == 1 and dilation == 1)
         if self.tiled:
             self.conv = TropicalConv2d(in_channels, out_channels, (1, kernel_size), stride=(1, stride),
                                        padding=(0, padding), dilation=(1, dilation), bias=bias, mode=mode,
-                                       chan=chan, params=params, dtype=dtype, fixed=fixed)
+                                       chan=chan, params=params, dtype=dtype, fixed=fixed, checkpoint=checkpoint)
         else:
             self.conv = TropicalConv3d(in_channels, out_channels, (1, 1, kernel_size), stride=(1, 1, stride),
                                        padding=(0, 0, padding), dilation=(1, 1, dilation), bias=bias, mode=mode,
-                                       chan=chan, params=params, dtype=dtype, fixed=fixed)
+                                       chan=chan, params=params, dtype=dtype, fixed=fixed, checkpoint=checkpoint)
 
-    def forward(self, x):                      # x: [N, C, L]
+    def forward(self, x, stored=None):         # x: [N, C, L]
         if self.tiled:
-            return self.conv(x.unsqueeze(2)).squeeze(2)
+            return self.conv(x.unsqueeze(2), stored).squeeze(2)
         # (reshapes, not slices: the gradient of a slice would be written into a zeroed copy)
         N, C, L = x.shape
-        y = self.conv(x.reshape(N, C, 1, 1, L))
+        y = self.conv(x.reshape(N, C, 1, 1, L), stored)
         return y.reshape(N, y.shape[1], y.shape[4])
 
 
@@ -631,3 +653,44 @@ class RMSNorm(nn.Module):
     def forward(self, x, residual=None):
         r = rms_norm(x, self.weight, residual, self.eps, checkpoint=self.checkpoint)
         return r.y if residual is None else (r.y, r.stream)
+
+
+class TropicalRecurrent1d(nn.Module):
+    """Gated recurrence whose candidates and gates one tropical convolution gives: [N, C_in, L] to 2 * channels signals,
+    the first half candidates, the second half gates, then gated_scan over them in place.  Takes TropicalConv1d's arguments.
+
+    gate_bias: initial bias of the gates (with bias=True): a new layer's states decay by sigmoid(gate_bias) a step.
+    checkpoint="q8": convolution and recurrence keep their inputs in 8 bits for the backward pass.
+    forward(x, h0, lengths, stored) gives y [N, channels, L'] and the last state, float32 [N, channels]."""
+
+    def __init__(self, in_channels, channels, kernel_size=3, stride=1, padding=1, dilation=1, bias=True, mode="compound",
+                 chan="default", params="2p", dtype="f32", gate_bias=2.0, checkpoint=None):
+        super().__init__()
+        self.channels, self.checkpoint = channels, checkpoint
+        self.conv = TropicalConv1d(in_channels, 2 * channels, kernel_size, stride, padding, dilation, bias, mode, chan,
+                                   params, dtype, checkpoint=checkpoint)
+        if bias:
+            nn.init.constant_(self.conv.conv.bias[channels:], gate_bias)
+
+    def forward(self, x, h0=None, lengths=None, stored=None):
+        return gated_scan(self.conv(x, stored), None, h0, lengths, self.checkpoint)
+
+
+class TropicalRecurrentBlock1d(nn.Module):
+    """Residual block of a network over long signals: RMS norm of the stream, tropical recurrence, and its output's addition
+    left to the next block's norm.  forward(x, residual=None) gives the branch and the stream, which the next block
+    (or a last RMSNorm) takes as its x and residual; the first block takes its input as x.  checkpoint="q8": the stream,
+    the convolution's input (in the norm's own 8-bit output) and the recurrence's are kept in 8 bits."""
+
+    def __init__(self, channels, kernel_size=3, padding=1, mode="compound", params="2p", dtype="f32", eps=1e-6,
+                 checkpoint=None):
+        super().__init__()
+        self.norm = RMSNorm(channels, eps, checkpoint)
+        self.rec = TropicalRecurrent1d(channels, channels, kernel_size, padding=padding, mode=mode, params=params, dtype=dtype,
+                                       checkpoint=checkpoint)
+
+    def forward(self, x, residual=None, lengths=None):
+        keep = self.norm.checkpoint is not None and torch.is_grad_enabled()
+        n = rms_norm(x, self.norm.weight, residual, self.norm.eps, "both" if keep else "same", self.norm.checkpoint)
+        y, _ = self.rec(n.y, None, lengths, n.q8)
+        return y, n.stream
