@@ -26,13 +26,6 @@ struct NormOut {
     uint8_t* ss;
 };
 
-// Writes one value of an 8-bit form whose block the warp's lanes hold; `at` is the lane's place in the row.
-__device__ __forceinline__ void q8_put(float v, int64_t row, int64_t at, int64_t inner, int8_t* codes, uint8_t* scales) {
-    const uint32_t byte = q8_scale_byte(__reduce_max_sync(~0u, magnitude_bits(v)));
-    if (at < q8_pitch(inner)) codes[row * q8_pitch(inner) + at] = (int8_t)q8_code(v, byte);
-    if ((threadIdx.x & 31) == 0 && at < inner) scales[row * q8_blocks(inner) + at / kQ8Block] = (uint8_t)byte;
-}
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int k = 16; k; k >>= 1) v += __shfl_xor_sync(~0u, v, k);
@@ -47,37 +40,33 @@ struct NormIn {
     const void *gy, *gs;
 };
 
-template <typename T>
-__device__ __forceinline__ float kept_value(const NormIn& k, int64_t row, int64_t at, int64_t inner) {
-    if (k.s) return to_f32(((const T*)k.s)[row * inner + at]);
-    return (float)k.sc[row * q8_pitch(inner) + at] * q8_unit(k.ss[row * q8_blocks(inner) + at / kQ8Block]);
-}
-
-
-// ---- V values of a thread that lie next to each other: 16 bytes, or one value where rows do not start on 16 bytes ----
+// ---- V values of a thread that lie next to each other: 16 bytes; 8 or one value where rows do not start on 16 bytes ----
 template <typename T, int V> struct Some { uint4 w; };
+template <> struct Some<__nv_bfloat16, 4> { uint2 w; };
 template <typename T> struct Some<T, 1> { T w; };
 
+template <typename T, int V> using Piece = decltype(Some<T, V>::w);
 template <typename T, int V> __device__ __forceinline__ Some<T, V> none_of() {
-    Some<T, V> s;
-    if constexpr (V == 1) s.w = zero_of<T>(); else s.w = make_uint4(0, 0, 0, 0);
-    return s;
+    if constexpr (V == 1) return {zero_of<T>()};
+    else return {};
 }
 template <typename T, int V> __device__ __forceinline__ Some<T, V> load_some(const void* p, int64_t at) {
-    Some<T, V> s;
-    if constexpr (V == 1) s.w = __ldg((const T*)p + at); else s.w = __ldg(reinterpret_cast<const uint4*>((const T*)p + at));
-    return s;
+    return {__ldg(reinterpret_cast<const Piece<T, V>*>((const T*)p + at))};
+}
+// What this thread has written before.
+template <typename T, int V> __device__ __forceinline__ Some<T, V> load_own(const void* p, int64_t at) {
+    return {*reinterpret_cast<const Piece<T, V>*>((const T*)p + at)};
 }
 template <typename T, int V> __device__ __forceinline__ void store_some(void* p, int64_t at, const Some<T, V>& s) {
-    if constexpr (V == 1) ((T*)p)[at] = s.w; else *reinterpret_cast<uint4*>((T*)p + at) = s.w;
+    *reinterpret_cast<Piece<T, V>*>((T*)p + at) = s.w;
 }
 template <typename T, int V> __device__ __forceinline__ void spread(const Some<T, V>& s, float (&v)[V]) {
     if constexpr (V == 1) v[0] = to_f32(s.w);
     else {
-        const uint32_t w[4] = {s.w.x, s.w.y, s.w.z, s.w.w};
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(&s.w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (V == 4) v[i] = __uint_as_float(w[i]);
+        for (int i = 0; i < (int)sizeof(s.w) / 4; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i]);
             else {
                 v[2 * i] = __uint_as_float(w[i] << 16);
                 v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
@@ -89,16 +78,15 @@ template <typename T, int V> __device__ __forceinline__ Some<T, V> gather(const 
     Some<T, V> s;
     if constexpr (V == 1) s.w = from_f32<T>(v[0]);
     else {
-        uint32_t w[4];
+        uint32_t* w = reinterpret_cast<uint32_t*>(&s.w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (V == 4) w[i] = __float_as_uint(v[i]);
+        for (int i = 0; i < (int)sizeof(s.w) / 4; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
             else {
                 const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
                 w[i] = *reinterpret_cast<const uint32_t*>(&p);
             }
         }
-        s.w = make_uint4(w[0], w[1], w[2], w[3]);
     }
     return s;
 }
@@ -518,26 +506,300 @@ __global__ void __launch_bounds__(256) norm_weight_sum_kernel(int C, int blocks,
     }
 }
 
+// ---- any channel count: the channels go in groups of what registers hold, and are read once more (from L2) after the sums ----
+template <typename T, int V, int WARPS, int R, bool RES, bool Q8>
+__global__ void __launch_bounds__(WARPS * 32, 2) norm_fwd_loop_kernel(const __grid_constant__ NormArgs a, const T* __restrict__ x,
+        const T* __restrict__ r, const float* __restrict__ w, const __grid_constant__ NormOut o) {
+    __shared__ float part[WARPS][kQ8Block], total[kQ8Block];
+    const Cols<V, WARPS> b;
+    const int64_t P = a.P, tiles = q8_blocks(P), pitch = q8_pitch(P), n = blockIdx.x / tiles, p0 = (blockIdx.x - n * tiles) * kQ8Block, p = p0 + b.lp * V;
+    const bool in = p < P;
+    const int64_t image = n * a.C * P;
+    T* sum = RES ? (T*)o.sum + image : nullptr;
+    const auto put = [&](const float (&v)[V], int c, int8_t* codes, uint8_t* scales) {
+        const int64_t row = n * a.C + c;
+        q8_put_some<V>(v, c < a.C && p < pitch, codes + row * pitch + p, b.lp == 0, scales + row * tiles + p0 / kQ8Block);
+    };
+    const int64_t step = b.kStep * P;
+    float sq[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sq[i] = 0.0f;
+    for (int base = b.c0; base - b.c0 < a.C; base += R * b.kStep) {
+        const int64_t at = base * P + p;
+        Some<T, V> s[R], t[RES ? R : 1];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int c = base + j * b.kStep;
+            s[j] = none_of<T, V>();
+            if (in && c < a.C) s[j] = load_some<T, V>(x + image, at + j * step);
+            if constexpr (RES) {
+                t[j] = none_of<T, V>();
+                if (in && c < a.C) t[j] = load_some<T, V>(r + image, at + j * step);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int c = base + j * b.kStep;
+            float v[V];
+            spread<T, V>(s[j], v);
+            if constexpr (RES) {
+                float u[V];
+                spread<T, V>(t[j], u);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] += u[i];
+                s[j] = gather<T, V>(v);
+                spread<T, V>(s[j], v);
+                if (in && c < a.C) store_some<T, V>(sum, at + j * step, s[j]);
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) sq[i] = fmaf(v[i], v[i], sq[i]);
+            if constexpr (Q8)
+                if (o.sc) put(v, c, o.sc, o.ss);
+        }
+    }
+    b.sum(sq, part, total, [&](float t, int i) {
+        const float rstd = 1.0f / sqrtf(t / (float)a.C + a.eps);
+        if (o.rstd && p0 + i < P) o.rstd[n * P + p0 + i] = rstd;
+        return rstd;
+    });
+    T* y = (T*)o.y + image;
+    for (int base = b.c0; base - b.c0 < a.C; base += R * b.kStep) {
+        const int64_t at = base * P + p;
+        Some<T, V> s[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int c = base + j * b.kStep;
+            s[j] = none_of<T, V>();
+            if (in && c < a.C) s[j] = RES ? load_own<T, V>(sum, at + j * step) : load_some<T, V>(x + image, at + j * step);
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int c = base + j * b.kStep;
+            const float wc = c < a.C ? __ldg(w + c) : 0.0f;
+            float v[V];
+            spread<T, V>(s[j], v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = in && c < a.C ? v[i] * sq[i] * wc : 0.0f;
+            if (o.y && in && c < a.C) store_some<T, V>(y, at + j * step, gather<T, V>(v));
+            if constexpr (Q8)
+                if (o.yc) put(v, c, o.yc, o.ys);
+        }
+    }
+}
+
+// gw_part as above; a block's sums grow there, each by one thread.
+template <typename T, int V, int WARPS, int R, bool RES, bool Q8>
+__global__ void __launch_bounds__(WARPS * 32, 2) norm_bwd_loop_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
+                                                                   T* __restrict__ gx, float* gw_part) {
+    __shared__ float part[WARPS][kQ8Block], total[kQ8Block];
+    const Cols<V, WARPS> b;
+    const int64_t P = a.P, tiles = q8_blocks(P), pitch = q8_pitch(P), all = tiles * a.N;
+    float* gw = gw_part ? gw_part + (int64_t)blockIdx.x * a.C : nullptr;
+    if (gw && b.lp == 0)
+        for (int c = b.c0; c < a.C; c += b.kStep) gw[c] = 0.0f;
+    for (int64_t tile = blockIdx.x; tile < all; tile += gridDim.x) {
+        const int64_t n = tile / tiles, p0 = (tile - n * tiles) * kQ8Block, p = p0 + b.lp * V;
+        const bool in = p < P;
+        const int64_t image = n * a.C * P, step = b.kStep * P;
+        Kept<T, V, Q8> s[R];
+        Some<T, V> dy[R];
+        const auto load = [&](int c, int64_t at, int j) {
+            s[j].none();
+            dy[j] = none_of<T, V>();
+            if (in && c < a.C) {
+                const int64_t row = n * a.C + c;
+                s[j].load((const T*)k.s + image + at, k.sc + row * pitch + p, k.ss + row * tiles + p0 / kQ8Block);
+                dy[j] = load_some<T, V>((const T*)k.gy + image, at);
+            }
+        };
+        float rstd[V], m[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            rstd[i] = in ? __ldg(k.rstd + n * P + p + i) : 0.0f;
+            m[i] = 0.0f;
+        }
+        for (int base = b.c0; base - b.c0 < a.C; base += R * b.kStep) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) load(base + j * b.kStep, base * P + p + j * step, j);
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const int c = base + j * b.kStep;
+                const float wc = c < a.C ? __ldg(k.w + c) : 0.0f;
+                float v[V], d[V], g = 0.0f;
+                s[j].values(v);
+                spread<T, V>(dy[j], d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float u = d[i] * (v[i] * rstd[i]);
+                    g += u;
+                    m[i] = fmaf(wc, u, m[i]);
+                }
+                if (gw) {
+#pragma unroll
+                    for (int d2 = 1; d2 < b.kLanes; d2 <<= 1) g += __shfl_xor_sync(~0u, g, d2);
+                    if (b.lp == 0 && c < a.C) gw[c] += g;
+                }
+            }
+        }
+        b.sum(m, part, total, [&](float u, int) { return u / (float)a.C; });
+        for (int base = b.c0; base - b.c0 < a.C; base += R * b.kStep) {
+            const int64_t at = base * P + p;
+            Some<T, V> ds[RES ? R : 1];
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const int c = base + j * b.kStep;
+                load(c, at + j * step, j);
+                if constexpr (RES) {
+                    ds[j] = none_of<T, V>();
+                    if (in && c < a.C) ds[j] = load_some<T, V>((const T*)k.gs + image, at + j * step);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                const int c = base + j * b.kStep;
+                const float wc = c < a.C ? __ldg(k.w + c) : 0.0f;
+                float v[V], d[V];
+                s[j].values(v);
+                spread<T, V>(dy[j], d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) d[i] = rstd[i] * (wc * d[i] - v[i] * rstd[i] * m[i]);
+                if constexpr (RES) {
+                    float e[V];
+                    spread<T, V>(ds[j], e);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) d[i] += e[i];
+                }
+                if (in && c < a.C) store_some<T, V>(gx + image, at + j * step, gather<T, V>(d));
+            }
+        }
+    }
+}
+
+// P = 1: a warp has a row, and its lanes V channels every 32 V.
+template <typename T, int V>
+__global__ void __launch_bounds__(128) norm_fwd_rows_loop_kernel(const __grid_constant__ NormArgs a, const T* __restrict__ x,
+        const T* __restrict__ r, const float* __restrict__ w, const __grid_constant__ NormOut o) {
+    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (n >= a.N) return;
+    const int lane = threadIdx.x & 31, top = (a.C + 31) & ~31;
+    const int64_t pitch = q8_pitch(a.C), nb = q8_blocks(a.C);
+    const auto put = [&](const float (&v)[V], int64_t c, int8_t* codes, uint8_t* scales) {
+        q8_put_some<V>(v, c < pitch, codes + n * pitch + c, c % kQ8Block == 0 && c < a.C, scales + n * nb + c / kQ8Block);
+    };
+    float sq = 0.0f;
+    for (int64_t base = 0; base < top; base += 32 * V) {
+        const int64_t c = base + lane * V;
+        float v[V];
+        Some<T, V> s = none_of<T, V>();
+        if (c < a.C) s = load_some<T, V>(x, n * a.C + c);
+        spread<T, V>(s, v);
+        if (r && c < a.C) {
+            float u[V];
+            spread<T, V>(load_some<T, V>(r, n * a.C + c), u);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += u[i];
+            s = gather<T, V>(v);
+            spread<T, V>(s, v);
+            store_some<T, V>(o.sum, n * a.C + c, s);
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) sq = fmaf(v[i], v[i], sq);
+        if (o.sc) put(v, c, o.sc, o.ss);
+    }
+    const float rstd = 1.0f / sqrtf(warp_sum(sq) / (float)a.C + a.eps);
+    if (o.rstd && lane == 0) o.rstd[n] = rstd;
+    for (int64_t base = 0; base < top; base += 32 * V) {
+        const int64_t c = base + lane * V;
+        float v[V];
+        Some<T, V> s = none_of<T, V>();
+        if (c < a.C) s = r ? load_own<T, V>(o.sum, n * a.C + c) : load_some<T, V>(x, n * a.C + c);
+        spread<T, V>(s, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = c < a.C ? v[i] * rstd * __ldg(w + c + i) : 0.0f;
+        if (o.y && c < a.C) store_some<T, V>(o.y, n * a.C + c, gather<T, V>(v));
+        if (o.yc) put(v, c, o.yc, o.ys);
+    }
+}
+
+template <typename T, int V, bool Q8>
+__global__ void __launch_bounds__(128) norm_bwd_rows_loop_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
+                                                                 T* __restrict__ gx) {
+    const int lane = threadIdx.x & 31;
+    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5), pitch = q8_pitch(a.C), nb = q8_blocks(a.C);
+    if (n >= a.N) return;
+    const float rstd = __ldg(k.rstd + n);
+    Kept<T, V, Q8> s;
+    float m = 0.0f;
+#pragma unroll 4
+    for (int64_t c = lane * V; c < a.C; c += 32 * V) {
+        float v[V], d[V];
+        s.load((const T*)k.s + n * a.C + c, k.sc + n * pitch + c, k.ss + n * nb + c / kQ8Block);
+        s.values(v);
+        spread<T, V>(load_some<T, V>(k.gy, n * a.C + c), d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) m = fmaf(__ldg(k.w + c + i), d[i] * (v[i] * rstd), m);
+    }
+    m = warp_sum(m) / (float)a.C;
+#pragma unroll 4
+    for (int64_t c = lane * V; c < a.C; c += 32 * V) {
+        float v[V], d[V];
+        s.load((const T*)k.s + n * a.C + c, k.sc + n * pitch + c, k.ss + n * nb + c / kQ8Block);
+        s.values(v);
+        spread<T, V>(load_some<T, V>(k.gy, n * a.C + c), d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] = rstd * (__ldg(k.w + c + i) * d[i] - v[i] * rstd * m);
+        if (k.gs) {
+            float e[V];
+            spread<T, V>(load_some<T, V>(k.gs, n * a.C + c), e);
+#pragma unroll
+            for (int i = 0; i < V; ++i) d[i] += e[i];
+        }
+        store_some<T, V>(gx, n * a.C + c, gather<T, V>(d));
+    }
+}
+
+// Its grad_weight: a thread has V channels and every gridDim.y-th row.  gw_part: [gridDim.y][C].
+template <typename T, int V, bool Q8>
+__global__ void __launch_bounds__(128) norm_bwd_rows_weight_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
+                                                                   float* __restrict__ gw_part) {
+    const int64_t c = ((int64_t)blockIdx.x * 128 + threadIdx.x) * V, pitch = q8_pitch(a.C), nb = q8_blocks(a.C);
+    if (c >= a.C) return;
+    float g[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) g[i] = 0.0f;
+#pragma unroll 4
+    for (int64_t n = blockIdx.y; n < a.N; n += gridDim.y) {
+        const float rstd = __ldg(k.rstd + n);
+        Kept<T, V, Q8> s;
+        float v[V], d[V];
+        s.load((const T*)k.s + n * a.C + c, k.sc + n * pitch + c, k.ss + n * nb + c / kQ8Block);
+        s.values(v);
+        spread<T, V>(load_some<T, V>(k.gy, n * a.C + c), d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = fmaf(d[i], v[i] * rstd, g[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) gw_part[(int64_t)blockIdx.y * a.C + c + i] = g[i];
+}
+
 // What a layer's kernels look like.
 struct NormPlan {
-    bool vec;                        // 16 bytes at a time
-    int form;                        // which of the kernels with all channels in registers; -1: none holds that many
-    int blocks;                      // of the backward pass
+    int vec;                         // values at a time: 16 bytes' worth, 4 or 1
+    int form;                        // which of the kernels with all channels in registers; -1: the one that goes over them in groups
+    int blocks, parts;               // blocks of the backward pass, and partial sums of grad_weight
 };
 
-// The kernels with P > 1, by V, warps and channels of a thread, from the smallest that holds all channels on.
+// The kernels with P > 1, by values at a time, warps, and channels of a thread, from the smallest that holds all channels on.
 template <typename F> void with_cols(std::integral_constant<int, 8>, int form, F f) {
     if (form == 0) f.template operator()<8, 4, 2>();
     else if (form == 1) f.template operator()<8, 4, 4>();
     else if (form == 2) f.template operator()<8, 8, 4>();
-    else if (form == 3) f.template operator()<8, 16, 4>();
-    else f.template operator()<8, 16, 8>();
+    else f.template operator()<8, 16, 4>();
 }
 template <typename F> void with_cols(std::integral_constant<int, 4>, int form, F f) {
-    if (form == 0) f.template operator()<4, 4, 2>();
-    else if (form == 1) f.template operator()<4, 4, 4>();
-    else if (form == 2) f.template operator()<4, 8, 4>();
-    else if (form == 3) f.template operator()<4, 16, 4>();
+    if (form == 0) f.template operator()<4, 4, 4>();
+    else if (form == 1) f.template operator()<4, 8, 4>();
+    else if (form == 2) f.template operator()<4, 16, 4>();
     else f.template operator()<4, 16, 8>();
 }
 template <typename F> void with_cols(std::integral_constant<int, 1>, int form, F f) {
@@ -547,152 +809,46 @@ template <typename F> void with_cols(std::integral_constant<int, 1>, int form, F
     else if (form == 3) f.template operator()<1, 16, 16>();
     else f.template operator()<1, 16, 32>();
 }
+// Calls f with the values at a time as a constant.
+template <typename T, typename F> void with_vec(int vec, F f) {
+    if constexpr (sizeof(T) == 2)
+        if (vec == 8) return f(std::integral_constant<int, 8>{});
+    if (vec == 4) f(std::integral_constant<int, 4>{});
+    else f(std::integral_constant<int, 1>{});
+}
 
 inline NormPlan plan_norm(const NormArgs& a, int dtype) {
-    const int V = dtype == TCONV_F32 ? 4 : 8;
     NormPlan p{};
-    p.vec = (a.P > 1 ? a.P : a.C) % V == 0;
+    const int64_t inner = a.P > 1 ? a.P : a.C;
+    const int most = dtype == TCONV_F32 ? 4 : 8;
+    p.vec = inner % most == 0 ? most : a.P > 1 && inner % 4 == 0 ? 4 : 1;
     p.form = -1;
     if (a.P == 1) {
-        const int least = p.vec ? 32 * V : 256;
+        const int least = p.vec > 1 ? 32 * p.vec : 256;
         for (int k = 0; p.form < 0 && (least << k) <= 1024; ++k)
             if (a.C <= least << k) p.form = k;
         p.blocks = (a.N + 3) / 4 < 148 * 2 ? (a.N + 3) / 4 : 148 * 2;
-    } else {
-        if ((int64_t)a.C * a.P >= (int64_t)1 << 30) return p;       // (offsets inside an image: 32 bits, in bytes)
-        const auto take = [&](auto v) {
-            for (int k = 4; k >= 0; --k)
-                with_cols(v, k, [&]<int VV, int WARPS, int R>() {
-                    if (a.C > VV * WARPS * R) return;
-                    p.form = k;
-                    const int64_t tiles = q8_blocks(a.P) * a.N, most = 148 * norm_resident(WARPS);
-                    p.blocks = (int)(tiles < most ? tiles : most);
-                });
-        };
-        if (!p.vec) take(std::integral_constant<int, 1>{});
-        else if (V == 4) take(std::integral_constant<int, 4>{});
-        else take(std::integral_constant<int, 8>{});
+        const int across = (a.C + 128 * p.vec - 1) / (128 * p.vec), splits = (148 * 8 + across - 1) / across;
+        p.parts = p.form >= 0 ? p.blocks : a.N < splits ? a.N : splits;
+        return p;
     }
+    int warps = 8;                   // of the kernel in groups
+    const auto take = [&](auto v) {
+        for (int k = decltype(v)::value == 1 ? 4 : 3; k >= 0; --k)
+            with_cols(v, k, [&]<int V, int WARPS, int R>() {
+                if (a.C > V * WARPS * R) return;
+                p.form = k;
+                warps = WARPS;
+            });
+    };
+    if ((int64_t)a.C * a.P < (int64_t)1 << 30) {       // (offsets inside an image: 32 bits, in bytes)
+        if (p.vec == 8) take(std::integral_constant<int, 8>{});
+        else if (p.vec == 4) take(std::integral_constant<int, 4>{});
+        else take(std::integral_constant<int, 1>{});
+    }
+    const int64_t tiles = q8_blocks(a.P) * a.N, resident = 148 * norm_resident(warps);
+    p.parts = p.blocks = (int)(tiles < resident ? tiles : resident);
     return p;
-}
-
-// Any channel count, P > 1: values are read again where they do not stay; a thread has one position, a warp 32 positions of one image, which are one 8-bit block of each channel.
-template <typename T>
-__global__ void __launch_bounds__(128) norm_fwd_cols_any_kernel(const __grid_constant__ NormArgs a, const T* __restrict__ x,
-        const T* __restrict__ r, const float* __restrict__ w, const __grid_constant__ NormOut o) {
-    const int64_t nb = q8_blocks(a.P), b = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (b >= nb * a.N) return;
-    const int64_t n = b / nb, p = (b - n * nb) * 32 + (threadIdx.x & 31);
-    const bool in = p < a.P;
-    const int64_t base = n * a.C * a.P + p;
-    T* sum = (T*)o.sum;
-    const auto value = [&](int c) {
-        if (!in) return 0.0f;
-        const int64_t i = base + c * a.P;
-        return r ? to_f32(from_f32<T>(to_f32(x[i]) + to_f32(r[i]))) : to_f32(x[i]);
-    };
-    float sq = 0.0f;
-    for (int c = 0; c < a.C; ++c) {
-        const float v = value(c);
-        sq = fmaf(v, v, sq);
-        if (r && in) sum[base + c * a.P] = from_f32<T>(v);
-        if (o.sc) q8_put(v, n * a.C + c, p, a.P, o.sc, o.ss);
-    }
-    const float rstd = 1.0f / sqrtf(sq / (float)a.C + a.eps);
-    if (o.rstd && in) o.rstd[n * a.P + p] = rstd;
-    for (int c = 0; c < a.C; ++c) {
-        const float v = in ? value(c) * rstd * w[c] : 0.0f;
-        if (o.y && in) ((T*)o.y)[base + c * a.P] = from_f32<T>(v);
-        if (o.yc) q8_put(v, n * a.C + c, p, a.P, o.yc, o.ys);
-    }
-}
-
-// Any channel count, P = 1: a warp has one row of C values.
-template <typename T>
-__global__ void __launch_bounds__(128) norm_fwd_rows_any_kernel(const __grid_constant__ NormArgs a, const T* __restrict__ x,
-        const T* __restrict__ r, const float* __restrict__ w, const __grid_constant__ NormOut o) {
-    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (n >= a.N) return;
-    const int lane = threadIdx.x & 31, top = (a.C + 31) & ~31;
-    T* sum = (T*)o.sum;
-    const auto value = [&](int c) {
-        if (c >= a.C) return 0.0f;
-        const int64_t i = n * a.C + c;
-        return r ? to_f32(from_f32<T>(to_f32(x[i]) + to_f32(r[i]))) : to_f32(x[i]);
-    };
-    float sq = 0.0f;
-    for (int c = lane; c < top; c += 32) {
-        const float v = value(c);
-        sq = fmaf(v, v, sq);
-        if (r && c < a.C) sum[n * a.C + c] = from_f32<T>(v);
-        if (o.sc) q8_put(v, n, c, a.C, o.sc, o.ss);
-    }
-    const float rstd = 1.0f / sqrtf(warp_sum(sq) / (float)a.C + a.eps);
-    if (o.rstd && lane == 0) o.rstd[n] = rstd;
-    for (int c = lane; c < top; c += 32) {
-        const float v = c < a.C ? value(c) * rstd * w[c] : 0.0f;
-        if (o.y && c < a.C) ((T*)o.y)[n * a.C + c] = from_f32<T>(v);
-        if (o.yc) q8_put(v, n, c, a.C, o.yc, o.ys);
-    }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(128) norm_bwd_cols_any_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
-                                                            T* __restrict__ gx) {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= a.P * a.N) return;
-    const int64_t n = i / a.P, p = i - n * a.P;
-    const float rstd = k.rstd[i];
-    const T *gy = (const T*)k.gy, *gs = (const T*)k.gs;
-    float m = 0.0f;
-    for (int c = 0; c < a.C; ++c) {
-        const int64_t row = n * a.C + c;
-        m = fmaf(k.w[c] * to_f32(gy[row * a.P + p]), kept_value<T>(k, row, p, a.P) * rstd, m);
-    }
-    m /= (float)a.C;
-    for (int c = 0; c < a.C; ++c) {
-        const int64_t row = n * a.C + c, at = row * a.P + p;
-        const float z = kept_value<T>(k, row, p, a.P) * rstd;
-        const float d = rstd * (k.w[c] * to_f32(gy[at]) - z * m);
-        gx[at] = from_f32<T>(gs ? d + to_f32(gs[at]) : d);
-    }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(128) norm_bwd_rows_any_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
-                                                            T* __restrict__ gx) {
-    const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (n >= a.N) return;
-    const int lane = threadIdx.x & 31;
-    const float rstd = k.rstd[n];
-    const T *gy = (const T*)k.gy, *gs = (const T*)k.gs;
-    float m = 0.0f;
-    for (int c = lane; c < a.C; c += 32)
-        m = fmaf(k.w[c] * to_f32(gy[n * a.C + c]), kept_value<T>(k, n, c, a.C) * rstd, m);
-    m = warp_sum(m) / (float)a.C;
-    for (int c = lane; c < a.C; c += 32) {
-        const int64_t at = n * a.C + c;
-        const float z = kept_value<T>(k, n, c, a.C) * rstd;
-        const float d = rstd * (k.w[c] * to_f32(gy[at]) - z * m);
-        gx[at] = from_f32<T>(gs ? d + to_f32(gs[at]) : d);
-    }
-}
-
-// grad_weight: one block per channel.
-template <typename T>
-__global__ void __launch_bounds__(256) norm_bwd_weight_any_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
-                                                              float* __restrict__ gw) {
-    __shared__ float red[256];
-    const int c = blockIdx.x;
-    const T* gy = (const T*)k.gy;
-    float m = 0.0f;
-    for (int64_t i = threadIdx.x; i < a.P * a.N; i += 256) {
-        const int64_t n = i / a.P, p = i - n * a.P, row = n * a.C + c;
-        const float v = a.P > 1 ? kept_value<T>(k, row, p, a.P) : kept_value<T>(k, n, c, a.C);
-        m = fmaf(to_f32(gy[row * a.P + p]), v * k.rstd[i], m);
-    }
-    m = block_sum(m, red);
-    if (threadIdx.x == 0) gw[c] = m;
 }
 
 }  // namespace tconv

@@ -12,10 +12,6 @@ constexpr int kQ8Block = 32;
 __host__ __device__ inline int64_t q8_pitch(int64_t inner) { return (inner + 7) / 8 * 8; }
 __host__ __device__ inline int64_t q8_blocks(int64_t inner) { return (inner + kQ8Block - 1) / kQ8Block; }
 
-// Magnitudes are compared as integers, so that a NaN, whose bits lie above those of infinity, is not dropped as fmaxf
-// would.
-__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-
 // Scale byte e + 127 of a block whose largest magnitude has the bits `top`: with amax = m * 2^k, 1 <= m < 2, it is k - 6
 // where m < 127.5 / 64 and k - 5 elsewhere; adding 2^16 carries into the exponent exactly where m's seven leading bits are
 // all ones, that is m >= 127.5 / 64.  Not below 1 (a normal 2^e with a normal inverse); 255 for infinities and NaN.
@@ -28,10 +24,6 @@ __device__ __forceinline__ uint32_t q8_scale_byte(uint32_t top) {
 __device__ __forceinline__ float q8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 // 2^e; infinity for 255, which makes every code 0 a NaN.
 __device__ __forceinline__ float q8_unit(uint32_t byte) { return __uint_as_float(byte << 23); }
-
-__device__ __forceinline__ int q8_code(float v, uint32_t byte) {
-    return byte == 255u ? 0 : __float2int_rn(v * q8_inverse(byte));
-}
 
 // Largest magnitude of N values; NaN if one of them is.
 template <int N> __device__ __forceinline__ float top_of(const float (&v)[N]) {

@@ -143,51 +143,59 @@ template <typename F> void with_flags(bool p, bool q, F f) {
 
 template <typename T>
 int norm_fwd_t(const NormArgs& a, const NormPlan& p, const void* x_, const void* r_, const float* w, const NormOut& o, cudaStream_t st) {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int kMostV = 16 / sizeof(T);
     const T *x = (const T*)x_, *r = (const T*)r_;
-    if (p.form < 0) {
-        if (a.P > 1) norm_fwd_cols_any_kernel<T><<<(unsigned)((q8_blocks(a.P) * a.N + 3) / 4), 128, 0, st>>>(a, x, r, w, o);
-        else norm_fwd_rows_any_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, x, r, w, o);
-    } else if (a.P == 1) {
+    if (a.P == 1) {
         const unsigned grid = (unsigned)((a.N + 3) / 4);
-        if (p.vec) with_reps<1, 32 / V>(p.form, [&]<int R>() { norm_fwd_rows_kernel<T, V, R><<<grid, 128, 0, st>>>(a, x, r, w, o); });
+        const bool vec = p.vec > 1;
+        if (p.form < 0) {
+            if (vec) norm_fwd_rows_loop_kernel<T, kMostV><<<grid, 128, 0, st>>>(a, x, r, w, o);
+            else norm_fwd_rows_loop_kernel<T, 1><<<grid, 128, 0, st>>>(a, x, r, w, o);
+        } else if (vec) with_reps<1, 32 / kMostV>(p.form, [&]<int R>() { norm_fwd_rows_kernel<T, kMostV, R><<<grid, 128, 0, st>>>(a, x, r, w, o); });
         else with_reps<8, 32>(p.form, [&]<int R>() { norm_fwd_rows_kernel<T, 1, R><<<grid, 128, 0, st>>>(a, x, r, w, o); });
     } else {
         const unsigned grid = (unsigned)(q8_blocks(a.P) * a.N);
-        const auto go = [&]<int VV, int WARPS, int R>() {
-            with_flags(r, o.yc || o.sc, [&]<bool RES, bool Q8>() { norm_fwd_cols_kernel<T, VV, WARPS, R, RES, Q8><<<grid, WARPS * 32, 0, st>>>(a, x, r, w, o); });
-        };
-        if (p.vec) with_cols(std::integral_constant<int, V>{}, p.form, go);
-        else with_cols(std::integral_constant<int, 1>{}, p.form, go);
+        with_vec<T>(p.vec, [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            with_flags(r, o.yc || o.sc, [&]<bool RES, bool Q8>() {
+                if (p.form < 0) norm_fwd_loop_kernel<T, V, 8, V == 1 ? 8 : 4, RES, Q8><<<grid, 256, 0, st>>>(a, x, r, w, o);
+                else with_cols(v, p.form, [&]<int, int WARPS, int R>() {
+                    norm_fwd_cols_kernel<T, V, WARPS, R, RES, Q8><<<grid, WARPS * 32, 0, st>>>(a, x, r, w, o);
+                });
+            });
+        });
     }
     return launched(1, "norm_fwd");
 }
 template <typename T> int norm_bwd_t(const NormArgs& a, const NormPlan& p, const NormIn& k, void* gx_, float* gw, float* part, cudaStream_t st) {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int kMostV = 16 / sizeof(T);
     T* gx = (T*)gx_;
     if (!gw) part = nullptr;
     const unsigned grid = (unsigned)p.blocks;
-    if (p.form < 0) {
-        if (a.P > 1) norm_bwd_cols_any_kernel<T><<<(unsigned)((a.P * a.N + 127) / 128), 128, 0, st>>>(a, k, gx);
-        else norm_bwd_rows_any_kernel<T><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, k, gx);
-    } else if (a.P == 1) {
-        const auto go = [&]<int VV, int R>() {
-            if (k.s) norm_bwd_rows_kernel<T, VV, R, false><<<grid, 128, 0, st>>>(a, k, gx, part);
-            else norm_bwd_rows_kernel<T, VV, R, true><<<grid, 128, 0, st>>>(a, k, gx, part);
+    if (a.P == 1) {
+        const auto go = [&]<int V, bool Q8>() {
+            if (p.form < 0) {
+                norm_bwd_rows_loop_kernel<T, V, Q8><<<(unsigned)((a.N + 3) / 4), 128, 0, st>>>(a, k, gx);
+                if (part) norm_bwd_rows_weight_kernel<T, V, Q8><<<dim3((unsigned)((a.C + 128 * V - 1) / (128 * V)), (unsigned)p.parts), 128, 0, st>>>(a, k, part);
+            } else if constexpr (V > 1) with_reps<1, 32 / V>(p.form, [&]<int R>() { norm_bwd_rows_kernel<T, V, R, Q8><<<grid, 128, 0, st>>>(a, k, gx, part); });
+            else with_reps<8, 32>(p.form, [&]<int R>() { norm_bwd_rows_kernel<T, 1, R, Q8><<<grid, 128, 0, st>>>(a, k, gx, part); });
         };
-        if (p.vec) with_reps<1, 32 / V>(p.form, [&]<int R>() { go.template operator()<V, R>(); });
-        else with_reps<8, 32>(p.form, [&]<int R>() { go.template operator()<1, R>(); });
+        if (p.vec > 1) k.s ? go.template operator()<kMostV, false>() : go.template operator()<kMostV, true>();
+        else k.s ? go.template operator()<1, false>() : go.template operator()<1, true>();
     } else {
-        const auto go = [&]<int VV, int WARPS, int R>() {
-            with_flags(k.gs, !k.s, [&]<bool RES, bool Q8>() { norm_bwd_cols_kernel<T, VV, WARPS, R, RES, Q8><<<grid, WARPS * 32, 0, st>>>(a, k, gx, part); });
-        };
-        if (p.vec) with_cols(std::integral_constant<int, V>{}, p.form, go);
-        else with_cols(std::integral_constant<int, 1>{}, p.form, go);
+        with_vec<T>(p.vec, [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            with_flags(k.gs, !k.s, [&]<bool RES, bool Q8>() {
+                if (p.form < 0) norm_bwd_loop_kernel<T, V, 8, V == 1 ? 8 : 4, RES, Q8><<<grid, 256, 0, st>>>(a, k, gx, part);
+                else with_cols(v, p.form, [&]<int, int WARPS, int R>() {
+                    norm_bwd_cols_kernel<T, V, WARPS, R, RES, Q8><<<grid, WARPS * 32, 0, st>>>(a, k, gx, part);
+                });
+            });
+        });
     }
-    const int rc = launched(1, "norm_bwd");
+    const int rc = launched(a.P == 1 && p.form < 0 && part ? 2 : 1, "norm_bwd");
     if (rc || !gw) return rc;
-    if (p.form >= 0) norm_weight_sum_kernel<8><<<(unsigned)((a.C + 31) / 32), 256, 0, st>>>(a.C, p.blocks, part, gw);
-    else norm_bwd_weight_any_kernel<T><<<(unsigned)a.C, 256, 0, st>>>(a, k, gw);
+    norm_weight_sum_kernel<8><<<(unsigned)((a.C + 31) / 32), 256, 0, st>>>(a.C, p.parts, part, gw);
     return launched(1, "norm_bwd");
 }
 
@@ -292,8 +300,7 @@ int tconv_scan_backward(const tconv_scan_desc_t* desc, const void* x, const void
 size_t tconv_norm_workspace_bytes(const tconv_norm_desc_t* desc) {
     NormArgs a;
     if (check_norm(desc, &a)) return 0;
-    const NormPlan p = plan_norm(a, desc->dtype);
-    return p.form >= 0 ? (size_t)p.blocks * a.C * sizeof(float) : 0;
+    return (size_t)plan_norm(a, desc->dtype).parts * a.C * sizeof(float);
 }
 
 int tconv_norm_forward(const tconv_norm_desc_t* desc, const void* x, const void* residual, const float* weight, void* sum, void* y,
