@@ -254,6 +254,7 @@ int tconv_dw_backward(const tconv_desc_t *desc, const void *x, const void *w, co
 /*
  * Operators around the one-dimensional layers of residual networks over long signals, and activations kept in
  * 8 bits.  Offsets are 64 bits wide.  Inputs may hold infinities and NaN: they reach the outputs that depend on them.
+ * Outputs overlap neither inputs nor each other, but for h_last where it is said.
  *
  * Activations in 8 bits.  A tensor is rows x inner values (inner: the axes behind the channels; the channels
  * where nothing is behind them).  Along a row, blocks of 32 values (the last one may be shorter) share a power

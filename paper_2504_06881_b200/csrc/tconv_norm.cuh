@@ -587,14 +587,18 @@ __global__ void __launch_bounds__(WARPS * 32, 2) norm_fwd_loop_kernel(const __gr
     }
 }
 
-// gw_part as above; a block's sums grow there, each by one thread.
+// gw_part as above; a block's sums grow in shared memory where they fit (in place a sum waited for its last write at every
+// tile: 151 us against 116 for 8 x 1024 x 8192 bf16), else there, each by one thread.
+constexpr int kNormShared = 8192;
 template <typename T, int V, int WARPS, int R, bool RES, bool Q8>
 __global__ void __launch_bounds__(WARPS * 32, 2) norm_bwd_loop_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ NormIn k,
                                                                    T* __restrict__ gx, float* gw_part) {
     __shared__ float part[WARPS][kQ8Block], total[kQ8Block];
     const Cols<V, WARPS> b;
     const int64_t P = a.P, tiles = q8_blocks(P), pitch = q8_pitch(P), all = tiles * a.N;
-    float* gw = gw_part ? gw_part + (int64_t)blockIdx.x * a.C : nullptr;
+    extern __shared__ float own[];
+    float* out = gw_part ? gw_part + (int64_t)blockIdx.x * a.C : nullptr;
+    float* gw = gw_part && a.C <= kNormShared ? own : out;
     if (gw && b.lp == 0)
         for (int c = b.c0; c < a.C; c += b.kStep) gw[c] = 0.0f;
     for (int64_t tile = blockIdx.x; tile < all; tile += gridDim.x) {
@@ -673,6 +677,8 @@ __global__ void __launch_bounds__(WARPS * 32, 2) norm_bwd_loop_kernel(const __gr
             }
         }
     }
+    if (gw != out && b.lp == 0)
+        for (int c = b.c0; c < a.C; c += b.kStep) out[c] = gw[c];
 }
 
 // P = 1: a warp has a row, and its lanes V channels every 32 V.

@@ -124,7 +124,7 @@ int scan_any(const ScanArgs& a, const ScanPlan& p, const IO& io, int dtype, bool
 int check_norm(const tconv_norm_desc_t* d, NormArgs* a) {
     if (!d || d->N <= 0 || d->C <= 0 || d->P <= 0 || (d->dtype != TCONV_F32 && d->dtype != TCONV_BF16) || !(d->eps >= 0))
         return TCONV_ERR_INVALID_ARG;
-    if ((int64_t)d->N * d->C > kMost / d->P || (int64_t)d->N > (int64_t)INT32_MAX * 32 / d->P) return TCONV_ERR_TOO_LARGE;
+    if ((int64_t)d->N * d->C > kMost / d->P || (int64_t)d->N > (int64_t)INT32_MAX / q8_blocks(d->P)) return TCONV_ERR_TOO_LARGE;
     *a = NormArgs{d->N, d->C, d->P, d->eps};
     return TCONV_OK;
 }
@@ -186,7 +186,7 @@ template <typename T> int norm_bwd_t(const NormArgs& a, const NormPlan& p, const
         with_vec<T>(p.vec, [&](auto v) {
             constexpr int V = decltype(v)::value;
             with_flags(k.gs, !k.s, [&]<bool RES, bool Q8>() {
-                if (p.form < 0) norm_bwd_loop_kernel<T, V, 8, V == 1 ? 8 : 4, RES, Q8><<<grid, 256, 0, st>>>(a, k, gx, part);
+                if (p.form < 0) norm_bwd_loop_kernel<T, V, 8, V == 1 ? 8 : 4, RES, Q8><<<grid, 256, a.C <= kNormShared ? a.C * sizeof(float) : 0, st>>>(a, k, gx, part);
                 else with_cols(v, p.form, [&]<int, int WARPS, int R>() {
                     norm_bwd_cols_kernel<T, V, WARPS, R, RES, Q8><<<grid, WARPS * 32, 0, st>>>(a, k, gx, part);
                 });

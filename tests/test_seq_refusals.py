@@ -76,6 +76,7 @@ def test_norm_refusals():
                 tseq.norm_desc(2, 8, 5, eps=float("nan"))):
         assert fwd(bad) == -1 and bwd(bad) == -1 and tseq.tconv_norm_workspace_bytes(bad) == 0
     assert fwd(tseq.norm_desc(1 << 30, 1 << 30, 5)) == -7
+    assert fwd(tseq.norm_desc((1 << 30) + 1, 1, 33)) == -7             # more blocks of 32 positions than a launch counts
     assert fwd(ok, x=0) == -1 and fwd(ok, w=0) == -1 and fwd(ok, y=0) == -1
     assert fwd(ok, yc=0x100) == -1 and fwd(ok, ss=0x100) == -1
     assert fwd(ok, r=0x100) == -1 and fwd(ok, sum=0x100) == -1          # a residual and its sum go together
