@@ -52,16 +52,51 @@ struct ScanBwd {
     float* gh0;
 };
 
+// Two values an instruction: a thread's positions go in pairs (i, i + 4), its two halves side by side.
+struct Pair {
+    float lo, hi;
+};
+__device__ __forceinline__ unsigned long long bits(Pair a) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.lo), "f"(a.hi));
+    return r;
+}
+__device__ __forceinline__ Pair pair(unsigned long long r) {
+    Pair a;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a.lo), "=f"(a.hi) : "l"(r));
+    return a;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return pair(r);
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return pair(r);
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return pair(r);
+}
+
 struct Gate {
-    float f, u;                      // 1 / (1 + e^-g) and 1 - f
+    Pair f, u;                       // 1 / (1 + e^-g) and 1 - f
 };
 // e^-g as 2^(-g log2 e), held to 2^115 (a lesser f adds nothing to a sum in fp32), so that u = e^-g * f stays finite; NaN passes.
-__device__ __forceinline__ Gate gate_of(float g) {
-    float m, e, f;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(g * -1.4426950408889634f), "f"(115.0f));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(m));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(1.0f + e));
-    return {f, e * f};
+__device__ __forceinline__ Gate gate_of(Pair g) {
+    const Pair t = mul2(g, {-1.4426950408889634f, -1.4426950408889634f});
+    Pair m, e, f;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(m.lo) : "f"(t.lo), "f"(115.0f));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(m.hi) : "f"(t.hi), "f"(115.0f));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.lo) : "f"(m.lo));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.hi) : "f"(m.hi));
+    const Pair d = add2(e, {1.0f, 1.0f});
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f.lo) : "f"(d.lo));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f.hi) : "f"(d.hi));
+    return {f, mul2(e, f)};
 }
 
 __device__ __forceinline__ uint32_t row_length(const ScanArgs& a, int64_t n) {
@@ -277,6 +312,18 @@ struct Map {
 };
 __device__ __forceinline__ Map then(Map first, Map second) { return {first.P * second.P, fmaf(second.P, first.B, second.B)}; }
 __device__ __forceinline__ float apply(Map m, float h) { return fmaf(m.P, h, m.B); }
+struct Halves {
+    Map lo, hi;                      // of a thread's first and last four positions
+};
+__device__ __forceinline__ Halves chain(const Pair (&f)[4], const Pair (&b)[4]) {
+    Pair P = f[0], B = b[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+        B = fma2(f[i], B, b[i]);
+        P = mul2(P, f[i]);
+    }
+    return {{P.lo, B.lo}, {P.hi, B.hi}};
+}
 
 // Joins the maps of the G threads of a row in order (UP: from the first thread on): a thread gets the map of all before it;
 // `all` (valid in the last thread) is the whole group's.  The shuffle's own predicate says whether there is a thread that far.
@@ -424,7 +471,8 @@ scan_fwd_kernel(const __grid_constant__ ScanArgs a,
     int turn = 0;
     const auto step = [&]<bool WHOLE>(uint32_t k) {
         const uint32_t chunk = k + (MODE == kBlock ? warp : 0), here = chunk * kScanChunk + sub * kScanVec;
-        float x[8], g[8], f[8], b[8];
+        float x[8], g[8];
+        Pair f[4], b[4];
         if constexpr (kChunks) {
             ring_wait();
             rx.take(turn, x);
@@ -442,15 +490,15 @@ scan_fwd_kernel(const __grid_constant__ ScanArgs a,
                 if (i >= live) x[i] = g[i] = 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const Gate q = gate_of(g[i]);
+        for (int i = 0; i < 4; ++i) {
+            const Gate q = gate_of(Pair{g[i], g[i + 4]});
             f[i] = q.f;
-            b[i] = __fmul_rn(q.u, x[i]);
-            if (!WHOLE && i >= live) { f[i] = 1.0f; b[i] = 0.0f; }
+            b[i] = mul2(q.u, {x[i], x[i + 4]});
+            if (!WHOLE && i >= live) { f[i].lo = 1.0f; b[i].lo = 0.0f; }
+            if (!WHOLE && i + 4 >= live) { f[i].hi = 1.0f; b[i].hi = 0.0f; }
         }
-        Map m{f[0], b[0]};
-#pragma unroll
-        for (int i = 1; i < 8; ++i) m = then(m, {f[i], b[i]});
+        const Halves halves = chain(f, b);
+        const Map m = then(halves.lo, halves.hi);
         [[maybe_unused]] Map all, all_q, before;
         if constexpr (MODE == kJoin) all = warp_join(m);
         else {
@@ -470,14 +518,17 @@ scan_fwd_kernel(const __grid_constant__ ScanArgs a,
                     }
                 }
             }
-            Map mq{1.0f, 0.0f};
+            Pair fq[4], bq[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const Gate q = gate_of(g[i]);
-                const Map one{q.f, __fmul_rn(q.u, x[i])};
-                if (WHOLE) mq = i ? then(mq, one) : one;
-                else if (i < live) mq = then(mq, one);
+            for (int i = 0; i < 4; ++i) {
+                const Gate q = gate_of(Pair{g[i], g[i + 4]});
+                fq[i] = q.f;
+                bq[i] = mul2(q.u, {x[i], x[i + 4]});
+                if (!WHOLE && i >= live) { fq[i].lo = 1.0f; bq[i].lo = 0.0f; }
+                if (!WHOLE && i + 4 >= live) { fq[i].hi = 1.0f; bq[i].hi = 0.0f; }
             }
+            const Halves halves_q = chain(fq, bq);
+            const Map mq = then(halves_q.lo, halves_q.hi);
             if constexpr (G == 32) all_q = warp_join(mq);
             else {
                 before_me<G, true>(mq, all_q);
@@ -502,12 +553,14 @@ scan_fwd_kernel(const __grid_constant__ ScanArgs a,
                 if constexpr (Q8) hq = apply(all_q, hq);
             }
             if (states && sub == 0 && (WHOLE || (mine && chunk < a.chunks))) states[chunk] = Q8 ? start_q : start;
-            float v = apply(before, start);
+            const float v0 = apply(before, start);
+            Pair v{v0, apply(halves.lo, v0)};
             float y[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v = fmaf(f[i], v, b[i]);
-                y[i] = WHOLE || i < live ? v : 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                v = fma2(f[i], v, b[i]);
+                y[i] = WHOLE || i < live ? v.lo : 0.0f;
+                y[i + 4] = WHOLE || i + 4 < live ? v.hi : 0.0f;
             }
             if constexpr (!kChunks) put_eight<T, ACC>(py, here, L, y);
             else if (WHOLE || chunk < a.chunks) put_chunk<T, ACC, WHOLE>(py + (int64_t)chunk * kScanChunk, L - chunk * kScanChunk, y, stage);
@@ -640,7 +693,8 @@ scan_bwd_kernel(const __grid_constant__ ScanArgs a,
     int turn = 0;
     const auto step = [&]<bool WHOLE>() {
         const uint32_t chunk = chunk_of(j), here = chunk * kScanChunk + sub * kScanVec;
-        float x[8], g[8], d[8], f[8], u[8];
+        float x[8], g[8], d[8];
+        Pair f[4], u[4];
         if constexpr (kChunks) {
             ring_wait();
             ry.take(turn, d);
@@ -663,27 +717,35 @@ scan_bwd_kernel(const __grid_constant__ ScanArgs a,
         if (kChunks && j > 0) fetch_kept(j - 1);
         const int live = WHOLE ? 8 : end <= here ? 0 : (int)min(end - here, (uint32_t)kScanVec);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const Gate q = gate_of(g[i]);
+        for (int i = 0; i < 4; ++i) {
+            const Gate q = gate_of(Pair{g[i], g[i + 4]});
             f[i] = q.f;
             u[i] = q.u;
-            if (!WHOLE && i >= live) { f[i] = 1.0f; u[i] = 0.0f; x[i] = 0.0f; d[i] = 0.0f; }
+            if (!WHOLE && i >= live) { f[i].lo = 1.0f; u[i].lo = 0.0f; x[i] = 0.0f; d[i] = 0.0f; }
+            if (!WHOLE && i + 4 >= live) { f[i].hi = 1.0f; u[i].hi = 0.0f; x[i + 4] = 0.0f; d[i + 4] = 0.0f; }
         }
         [[maybe_unused]] Map all;
-        Map back{f[7], __fmul_rn(f[7], d[7])};
+        Pair P = f[3], Q = mul2(f[3], {d[3], d[7]});
 #pragma unroll
-        for (int i = 6; i >= 0; --i) back = {back.P * f[i], __fmul_rn(f[i], __fadd_rn(d[i], back.B))};
+        for (int i = 2; i >= 0; --i) {
+            Q = mul2(f[i], add2({d[i], d[i + 4]}, Q));
+            P = mul2(P, f[i]);
+        }
+        const Map back_hi{P.hi, Q.hi}, back = then(back_hi, {P.lo, Q.lo});
         if constexpr (MODE == kJoin) {
             // (from the end of the row on: the maps of later lanes come first)
             const Map mirrored{__shfl_sync(~0u, back.P, 31 - lane), __shfl_sync(~0u, back.B, 31 - lane)};
             total = then(total, warp_join(mirrored));
         } else {
-            float b[8];
+            Pair b[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] = __fmul_rn(u[i], x[i]);
-            Map m{back.P, b[0]}, unused;
+            for (int i = 0; i < 4; ++i) b[i] = mul2(u[i], {x[i], x[i + 4]});
+            Pair B = b[0];
 #pragma unroll
-            for (int i = 1; i < 8; ++i) m.B = fmaf(f[i], m.B, b[i]);
+            for (int i = 1; i < 4; ++i) B = fma2(f[i], B, b[i]);
+            const Map lo{P.lo, B.lo};
+            [[maybe_unused]] Map unused;
+            const Map m{back.P, fmaf(P.hi, B.lo, B.hi)};
             const Map behind = before_me<G, false>(back, all), before = before_me<G, true>(m, unused);
             all = of_last<G, false>(all);
             float start = E;
@@ -692,20 +754,23 @@ scan_bwd_kernel(const __grid_constant__ ScanArgs a,
                 __syncthreads();
                 block_carry<false>(shared[turn], warp, warps, E, start, E);
             } else E = apply(all, E);
-            float v = apply(before, first), w = apply(behind, start);
+            const float v0 = apply(before, first), w7 = apply(behind, start);
+            Pair v{v0, apply(lo, v0)}, w{apply(back_hi, w7), w7};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float prev = v;
-                v = fmaf(f[i], v, b[i]);
-                b[i] = prev - x[i];
+            for (int i = 0; i < 4; ++i) {
+                const Pair prev = v;
+                v = fma2(f[i], v, b[i]);
+                b[i] = fma2({x[i], x[i + 4]}, {-1.0f, -1.0f}, prev);       // h_{t-1} - x_t
             }
 #pragma unroll
-            for (int i = 7; i >= 0; --i) {
-                const float D = __fadd_rn(d[i], w);
-                w = __fmul_rn(f[i], D);
-                x[i] = __fmul_rn(u[i], D);
-                g[i] = __fmul_rn(__fmul_rn(w, b[i]), u[i]);
-                if (!WHOLE && i >= live) x[i] = g[i] = 0.0f;
+            for (int i = 3; i >= 0; --i) {
+                const Pair D = add2({d[i], d[i + 4]}, w);
+                w = mul2(f[i], D);
+                const Pair dx = mul2(u[i], D), dg = mul2(mul2(w, b[i]), u[i]);
+                x[i] = WHOLE || i < live ? dx.lo : 0.0f;
+                x[i + 4] = WHOLE || i + 4 < live ? dx.hi : 0.0f;
+                g[i] = WHOLE || i < live ? dg.lo : 0.0f;
+                g[i + 4] = WHOLE || i + 4 < live ? dg.hi : 0.0f;
             }
             if constexpr (!kChunks) {
                 put_eight<T, ACC>(ox, here, L, x);
