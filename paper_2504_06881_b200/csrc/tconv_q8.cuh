@@ -195,20 +195,44 @@ __global__ void __launch_bounds__(256) q8_restore_any_kernel(int64_t rows, int64
     if (first >= total) return;
     I row = first / (I)inner, at = first - row * (I)inner;
     float v[8];
-    int q[8];
-    uint32_t b[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        q[i] = 0;
-        b[i] = 1;
-        if (first + i < total) {
-            q[i] = __ldg(codes + (int64_t)row * pitch + at);
-            b[i] = __ldg(scales + (int64_t)row * nb + at / kQ8Block);
+    if (inner >= 8) {
+        // eight values lie in one row, or in the end of one and the start of the next; in a row, in one block or two neighbours.
+        // Codes are read as the aligned eights around them (a row's codes are whole eights).
+        const int here = (int)(inner - at < 8 ? inner - at : 8);
+        const uint64_t* c = reinterpret_cast<const uint64_t*>(codes + (int64_t)row * pitch) + at / 8;
+        const int skip = 8 * (int)(at & 7);
+        uint64_t w = __ldg(c) >> skip;
+        if (skip && here > 8 - (int)(at & 7)) w |= __ldg(c + 1) << (64 - skip);
+        const uint8_t* s = scales + (int64_t)row * nb;
+        const I block = at / kQ8Block;
+        const int to_next = kQ8Block - (int)(at % kQ8Block);          // values left of the block
+        const uint32_t b0 = __ldg(s + block), b1 = to_next < here ? __ldg(s + block + 1) : b0;
+        uint32_t b2 = b0;
+        if (here < 8 && first + here < total) {
+            w = (w & ~(~0ull << 8 * here)) | __ldg(reinterpret_cast<const uint64_t*>(codes + (int64_t)(row + 1) * pitch)) << 8 * here;
+            b2 = __ldg(s + nb);
         }
-        if (++at == (I)inner) { at = 0; ++row; }
-    }
+        decode_four((uint32_t)w, 1.0f, v);
+        decode_four((uint32_t)(w >> 32), 1.0f, v + 4);
+        const float u0 = q8_unit(b0), u1 = q8_unit(b1), u2 = q8_unit(b2);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)q[i] * q8_unit(b[i]);
+        for (int i = 0; i < 8; ++i) v[i] *= i >= here ? u2 : i >= to_next ? u1 : u0;
+    } else {
+        int q[8];
+        uint32_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q[i] = 0;
+            b[i] = 1;
+            if (first + i < total) {
+                q[i] = __ldg(codes + (int64_t)row * pitch + at);
+                b[i] = __ldg(scales + (int64_t)row * nb + at / kQ8Block);
+            }
+            if (++at == (I)inner) { at = 0; ++row; }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)q[i] * q8_unit(b[i]);
+    }
     if (first + 8 <= total) write_eight(x + first, v);
     else
 #pragma unroll
