@@ -5,8 +5,10 @@
 // its 32 threads' pairs by shuffles (a chunk of 256 positions), then every thread runs its 8 positions once more from its true
 // state.  Rows go to warps; where there are fewer rows than keep the GPU busy, a block's warps take a row's chunks in turn and
 // hand the state round, and where there are very few a first kernel joins the maps of parts of a row.
-// HBM would be the bound (6 bytes a position forward in bf16, 10 backward), but at some 25 and 40 instructions a position
-// the issue slots are nearly as short, so that what is not arithmetic is kept out of the whole chunks' way.
+// HBM is the bound (6 bytes a position forward in bf16, 10 backward) where rows start on 16 bytes: 64 x 256 x 8192 bf16, half of
+// it live, takes 87 and 156 us, 5.8 TB/s.  At 29 and 50 instructions a position the issue slots and, for odd 16-bit rows, the
+// shared-memory path are nearly as short (32 x 128 x 3981: 29 and 40 us, 3.4 and 4.1 TB/s), so that whatever is not arithmetic
+// is kept out of the whole chunks' way.
 #pragma once
 #include "tconv_q8.cuh"
 
