@@ -213,10 +213,13 @@ __global__ void __launch_bounds__(WARPS * 32) norm_fwd_cols_kernel(const __grid_
             if (j < live) store_some<T, V>(sum, at + j * step, s[j]);
         }
     }
+    const uint32_t code_at = b.c0 * pitch + p, scale_at = b.c0 * tiles + p0 / kQ8Block;      // (inside the image too)
     const auto put = [&](const float (&v)[V], int j, int8_t* codes, uint8_t* scales) {
-        const int64_t row = (int64_t)n * a.C + b.c0 + j * b.kStep;
-        q8_put_some<V>(v, j < have && p < pitch, codes + row * pitch + p, b.lp == 0, scales + row * tiles + p0 / kQ8Block);
+        q8_put_some<V>(v, j < have && p < pitch, codes + (code_at + j * b.kStep * pitch), b.lp == 0, scales + (scale_at + j * b.kStep * tiles));
     };
+    const int64_t row0 = (int64_t)n * a.C;
+    int8_t *sc = o.sc + row0 * pitch, *yc = o.yc + row0 * pitch;
+    uint8_t *ss = o.ss + row0 * tiles, *ys = o.ys + row0 * tiles;
     float sq[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sq[i] = 0.0f;
@@ -227,7 +230,7 @@ __global__ void __launch_bounds__(WARPS * 32) norm_fwd_cols_kernel(const __grid_
 #pragma unroll
         for (int i = 0; i < V; ++i) sq[i] = fmaf(v[i], v[i], sq[i]);
         if constexpr (Q8)
-            if (o.sc) put(v, j, o.sc, o.ss);
+            if (o.sc) put(v, j, sc, ss);
     }
     b.sum(sq, part, total, [&](float t, uint32_t i) {
         const float rstd = 1.0f / sqrtf(t / (float)a.C + a.eps);
@@ -248,7 +251,7 @@ __global__ void __launch_bounds__(WARPS * 32) norm_fwd_cols_kernel(const __grid_
                 if (j >= live)       // (a row's end, where 0 * NaN must not poison the block)
 #pragma unroll
                     for (int i = 0; i < V; ++i) v[i] = 0.0f;
-                put(v, j, o.yc, o.ys);
+                put(v, j, yc, ys);
             }
         } else if (j < live) store_some<T, V>(y, at + j * step, gather<T, V>(v));
     }
