@@ -661,7 +661,8 @@ class TropicalRecurrent1d(nn.Module):
 
     gate_bias: initial bias of the gates (with bias=True): a new layer's states decay by sigmoid(gate_bias) a step.
     checkpoint="q8": convolution and recurrence keep their inputs in 8 bits for the backward pass.
-    forward(x, h0, lengths, stored) gives y [N, channels, L'] and the last state, float32 [N, channels]."""
+    forward(x, h0, lengths, stored) gives y [N, channels, L'] and the last state, float32 [N, channels]; lengths counts
+    output positions (the convolution itself sees all of x), stored is x's Q8 where it is there already."""
 
     def __init__(self, in_channels, channels, kernel_size=3, stride=1, padding=1, dilation=1, bias=True, mode="compound",
                  chan="default", params="2p", dtype="f32", gate_bias=2.0, checkpoint=None):
