@@ -4,7 +4,7 @@
 // holds all channels of its positions in registers from the one read to the write, and what has to be summed over channels
 // goes through shared memory once.  The backward kernels run as many blocks as are resident and keep grad_weight's sums in
 // registers over all their positions; a second kernel adds the blocks' sums in order.  8 x 256 x 128 x 256 bf16 with an 8-bit output
-// takes 106 us forward (5.7 TB/s) and 101 backward (5.3); 32 x 128 x 3981 fp32, value by value, 48 and 54 us (5.5 and 4.8 TB/s).
+// takes 106 us forward (5.7 TB/s) and 101 backward (5.3); 32 x 128 x 3981 fp32, value by value, 45 and 53 us (5.8 and 4.9 TB/s).
 #pragma once
 #include "tconv_q8.cuh"
 
