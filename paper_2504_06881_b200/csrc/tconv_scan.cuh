@@ -808,7 +808,9 @@ scan_bwd_kernel(const __grid_constant__ ScanArgs a,
     }
 }
 
-// How a row's positions are shared out.
+// How a row's positions are shared out: short rows several to a warp; a row to a warp where there are rows enough; a block's warps
+// in turn on a row, up to eight, in one pass; below that parts of a row, a warp each, in two passes (24 rows of 400001 positions:
+// 27 us against 52 with the parts in blocks whose warps take turns).
 struct ScanPlan {
     int g, warps, parts;             // threads of a row (1, 4, 16, 32); warps of a block on one row; parts of a row, a warp each
     uint32_t per_part;               // chunks
