@@ -258,12 +258,14 @@ int tconv_dw_backward(const tconv_desc_t *desc, const void *x, const void *w, co
  *
  * Activations in 8 bits.  A tensor is rows x inner values (inner: the axes behind the channels; the channels
  * where nothing is behind them).  Along a row, blocks of 32 values (the last one may be shorter) share a power
- * of two 2^e: the smallest e >= -126 with every magnitude of the block below 127.5 * 2^e.
+ * of two 2^e: the smallest e >= -126 with every magnitude of the block below 127.5 * 2^e, but 121 at most.
  *   codes  int8  [rows][pitch], pitch = inner rounded up to a multiple of 8: x * 2^-e rounded to the nearest
- *                whole number, halves to even (never beyond +-127); the padding of a row is 0;
+ *                whole number, halves to even, held to +-127 (which matters at e = 121 alone); the padding of a
+ *                row is 0;
  *   scales uint8 [rows][ceil(inner / 32)]: e + 127.
- * A value stands for code * 2^e, exact in float and in bf16, within half of 2^e of the original.  A block with a
- * NaN or an infinity has scale 255 and codes 0, and restores to NaN throughout.
+ * A value stands for code * 2^e, finite and exact in float and in bf16, within half of 2^e of the original;
+ * magnitudes from 127.5 * 2^121 (3.3895e38) on restore to 127 * 2^121 (3.3762e38), within 2^121 of the original.
+ * A block with a NaN or an infinity has scale 255 and codes 0, and restores to NaN throughout.
  */
 size_t tconv_q8_codes_bytes(int64_t rows, int64_t inner);
 size_t tconv_q8_scales_bytes(int64_t rows, int64_t inner);

@@ -15,11 +15,13 @@ __host__ __device__ inline int64_t q8_blocks(int64_t inner) { return (inner + kQ
 
 // Scale byte e + 127 of a block whose largest magnitude has the bits `top`: with amax = m * 2^k, 1 <= m < 2, it is k - 6
 // where m < 127.5 / 64 and k - 5 elsewhere; adding 2^16 carries into the exponent exactly where m's seven leading bits are
-// all ones, that is m >= 127.5 / 64.  Not below 1 (a normal 2^e with a normal inverse); 255 for infinities and NaN.
+// all ones, that is m >= 127.5 / 64.  Not below 1 (a normal 2^e with a normal inverse), nor above kQ8Top (at e = 122 code 64 would
+// stand for 2^128, which neither type has); 255 for infinities and NaN.
+constexpr uint32_t kQ8Top = 121 + 127;
 __device__ __forceinline__ uint32_t q8_scale_byte(uint32_t top) {
     if (top >= 0x7f800000u) return 255u;
     const int e = (int)((top + 0x10000u) >> 23) - 6;
-    return (uint32_t)(e < 1 ? 1 : e);
+    return (uint32_t)min(max(e, 1), (int)kQ8Top);
 }
 // 2^-e.  A poisoned block has codes 0.
 __device__ __forceinline__ float q8_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
@@ -44,15 +46,16 @@ template <int G> __device__ __forceinline__ uint32_t block_scale(const float (&v
     }
     return q8_scale_byte(top);
 }
-// v * 2^-e + 1.5 * 2^23: the sum's unit is 1, so that its low byte is the code, rounded half to even.
+// v * 2^-e + 1.5 * 2^23: the sum's unit is 1, so that its low byte is the code, rounded half to even.  With the largest unit
+// magnitudes from 127.5 units on, all below 128, are held to 127: less than a unit off.
 constexpr float kQ8Magic = 12582912.0f;
 template <int N> __device__ __forceinline__ void q8_round(const float (&v)[N], uint32_t byte, float (&r)[N]) {
     const float inv = q8_inverse(byte);
 #pragma unroll
     for (int i = 0; i < N; ++i) r[i] = fmaf(v[i], inv, kQ8Magic);
-    if (byte == 255u)
+    if (byte >= kQ8Top)
 #pragma unroll
-        for (int i = 0; i < N; ++i) r[i] = kQ8Magic;
+        for (int i = 0; i < N; ++i) r[i] = byte == 255u ? kQ8Magic : fminf(fmaxf(r[i], kQ8Magic - 127.0f), kQ8Magic + 127.0f);
 }
 __device__ __forceinline__ uint32_t four_codes(const float* r) {
     return __byte_perm(__byte_perm(__float_as_uint(r[0]), __float_as_uint(r[1]), 0x0040),

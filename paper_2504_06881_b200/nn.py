@@ -562,7 +562,8 @@ class TropicalConv1d(nn.Module):
 class Q8(NamedTuple):
     """A tensor kept in 8 bits: blocks of 32 values along a row (what lies behind the channel axis; the channels where
     nothing does) share a power of two, the smallest 2^e, e >= -126, with every magnitude below 127.5 * 2^e; a value is
-    code * 2^e.  A block with a NaN or an infinity restores to NaN.  codes: int8 [rows, inner rounded up to 8]; scales:
+    code * 2^e, finite for every finite value: e is 121 at most, and magnitudes from 127.5 * 2^121 on restore to
+    127 * 2^121.  A block with a NaN or an infinity restores to NaN.  codes: int8 [rows, inner rounded up to 8]; scales:
     uint8 [rows, blocks], e + 127."""
     codes: torch.Tensor
     scales: torch.Tensor
