@@ -276,7 +276,8 @@ int tconv_q8_restore(int64_t rows, int64_t inner, int dtype, const void *codes, 
 /*
  * Gated linear recurrence over signals [N][C][L], per row (n, c):
  *     h_t = f_t * h_{t-1} + (1 - f_t) * x_t,   f = 1 / (1 + exp(-gate)),   h_{-1} = h0 (NULL: 0),   y_t = h_t,
- * with gate, state and sums in fp32.  Positions of a row lie next to each other; x and gate have strides of their
+ * with gate, state and sums in fp32; a gate below -87.3 (f below 2^-126) is fully shut, f = 0, and one above 87.3
+ * fully open, 1 - f = 0.  Positions of a row lie next to each other; x and gate have strides of their
  * own between rows and between batch entries (elements), so that they can be parts of one tensor, and need only
  * be aligned to their type.  y and grad_y are dense, grad_x and grad_gate have dense rows and one stride between
  * batch entries.  lengths (int32 [N], NULL: all L; held to 0..L): from a row's length on its x and gate are not

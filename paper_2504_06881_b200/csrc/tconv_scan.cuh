@@ -87,18 +87,19 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
 struct Gate {
     Pair f, u;                       // 1 / (1 + e^-g) and 1 - f
 };
-// e^-g as 2^(-g log2 e), held to 2^115 (a lesser f adds nothing to a sum in fp32), so that u = e^-g * f stays finite; NaN passes.
+// With z = e^-|g| = 2^-|g log2 e|, z / (1 + z) is the smaller of f and u and 1 / (1 + z) the larger: nothing overflows, and a gate
+// at an end of its type gives 0 and 1.  Subnormal z count as 0 (a gate beyond -+87.3 is fully shut or open); NaN passes.
 __device__ __forceinline__ Gate gate_of(Pair g) {
-    const Pair t = mul2(g, {-1.4426950408889634f, -1.4426950408889634f});
-    Pair m, e, f;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(m.lo) : "f"(t.lo), "f"(115.0f));
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(m.hi) : "f"(t.hi), "f"(115.0f));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.lo) : "f"(m.lo));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.hi) : "f"(m.hi));
-    const Pair d = add2(e, {1.0f, 1.0f});
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f.lo) : "f"(d.lo));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f.hi) : "f"(d.hi));
-    return {f, mul2(e, f)};
+    const Pair t = mul2(g, {1.4426950408889634f, 1.4426950408889634f});
+    Pair z, large;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(z.lo) : "f"(-fabsf(t.lo)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(z.hi) : "f"(-fabsf(t.hi)));
+    const Pair d = add2(z, {1.0f, 1.0f});
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.lo) : "f"(d.lo));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.hi) : "f"(d.hi));
+    const Pair small = mul2(z, large);
+    const bool lo = g.lo < 0.0f, hi = g.hi < 0.0f;
+    return {{lo ? small.lo : large.lo, hi ? small.hi : large.hi}, {lo ? large.lo : small.lo, hi ? large.hi : small.hi}};
 }
 
 __device__ __forceinline__ uint32_t row_length(const ScanArgs& a, int64_t n) {

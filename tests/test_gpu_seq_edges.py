@@ -67,7 +67,7 @@ def test_scan_keeps_the_largest_finite_values(L, dtype):
         g = torch.full((1, 3, L), s * most, dtype=DT[dtype], device="cuda", requires_grad=True)
         y, last = tnn.gated_scan(x, g, checkpoint="q8")
         gx, gg = torch.autograd.grad(y, (x, g), gy)
-        assert torch.isfinite(gx).all() and (gg.abs() < 1e-30).all()
+        assert torch.isfinite(gx).all() and (gg == 0).all()
         if s > 0:
             assert (gx == 0).all() and (y == 0).all()
         else:
@@ -87,3 +87,79 @@ def test_norm_stores_the_largest_finite_values(shape, dtype):
     w = torch.full(shape[1:2], 3.4e38, device="cuda")
     o = tnn.rms_norm(x, w, eps=0.0, output="both")
     assert (o.q8.restore() == 127 * 2.0 ** 121).all() and (o.q8.scales == 248).all()
+
+
+# ---- gates ---------------------------------------------------------------------------------------------------
+EPS = ref.EPS
+LENGTHS = [1, 2, 8, 9, 33, 128, 129, 300, 3000]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", LENGTHS)
+def test_scan_shut_gates_and_large_states(L, dtype):
+    """A first state of any size behind a gate that is nearly or fully shut, then gates of 0.  f is the sigmoid down to 2^-126 and
+    zero below; e^-|g| is off by some (3 + |g|) steps of fp32 (the argument's rounding is |g| EPS, ex2 4 EPS), its sum, reciprocal and
+    product by 5 EPS more."""
+    most = float(torch.finfo(DT[dtype]).max)
+    gates = [-most, -200.0, -104.0, -88.0, -87.0, -85.0, -80.0, -79.0, -60.0, -10.0]
+    heights = [1.0, -1e30, 1e38, -3e38]
+    G, H = (a.reshape(1, -1) for a in np.meshgrid(gates, heights))
+    g = np.zeros((1, G.size, L))
+    g[..., 0] = G
+    gt, xt, h0 = _t(g, dtype), torch.ones(1, G.size, L, dtype=DT[dtype], device="cuda"), _t(H)
+    y, last = tnn.gated_scan(xt, gt, h0)
+    gv, hv = _np(gt)[..., 0], _np(h0)
+    e = np.exp(gv)
+    f = np.where(e / (1 + e) < 2.0 ** -126, 0.0, e / (1 + e))
+    h = f * hv + (1 - f)
+    off = np.abs(f * hv) * (2 * np.abs(np.where(f > 0, gv, 0.0)) + 12) * EPS + 8 * EPS * (np.abs(h) + 1)
+    for t in range(min(L, 40)):
+        if t:                                             # halving: exact gates, a few roundings
+            h, off = h / 2 + 0.5, off / 2 + 8 * EPS * (np.abs(h) + 1)
+        got = _np(y)[..., t]
+        assert (np.abs(got - h) <= off + ref.HALF[dtype] * (np.abs(h) + off)).all(), t
+    # a gate that is fully shut forgets: the same, bit for bit, from any state
+    shut = torch.full_like(gt, 0.0)
+    shut[..., L // 2] = -most
+    xr = _t(np.random.RandomState(L).standard_normal((1, G.size, L)), dtype)
+    a, la = tnn.gated_scan(xr, shut, h0)
+    b, lb = tnn.gated_scan(xr, shut, torch.zeros_like(h0))
+    shut[..., L // 2] = float("-inf")
+    c, lc = tnn.gated_scan(xr, shut, h0)
+    assert torch.equal(a[..., L // 2:], b[..., L // 2:]) and torch.equal(la, lb)
+    assert torch.equal(c, a) and torch.equal(lc, la) and torch.equal(a[..., L // 2], xr[..., L // 2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("checkpoint", [None, "q8"])
+@pytest.mark.parametrize("L", LENGTHS)
+def test_scan_gradients_at_extreme_gates(L, checkpoint, dtype):
+    """Rows cut by fully shut gates into stretches of three: gradients stay inside a stretch, and a shut gate has none of its own;
+    rows that are open throughout: y is the first state, x has no gradient and h0 has all of it."""
+    most = float(torch.finfo(DT[dtype]).max)
+    rs = np.random.RandomState(L)
+    x, gy = rs.standard_normal((2, 4, L)), rs.standard_normal((2, 4, L))
+    g = np.zeros((2, 4, L))
+    g[0, :, ::3] = -most if checkpoint else -np.inf
+    g[1] = most if checkpoint else np.inf                 # (kept in 8 bits an infinity poisons its block)
+    xt, gt, ht, gyt = _t(x, dtype, True), _t(g, dtype, True), _t(rs.standard_normal((2, 4)), grad=True), _t(gy, dtype)
+    y, last = tnn.gated_scan(xt, gt, ht, checkpoint=checkpoint)
+    gx, gg, gh = torch.autograd.grad(y, (xt, gt, ht), gyt)
+    assert torch.equal(y[1], ht[1, :, None].expand_as(y[1]).to(y.dtype)) and torch.equal(last[1], ht[1])
+    assert (gx[1] == 0).all() and (gg[1] == 0).all()
+    total = _np(gyt)[1].sum(-1)
+    assert (np.abs(_np(gh)[1] - total) <= (L + 8) * EPS * np.abs(_np(gyt)[1]).sum(-1)).all()
+    assert (gh[0] == 0).all() and (gg[0, :, ::3] == 0).all()
+    # D_t = dy_t + D_{t+1} / 2 inside a stretch; u is 1 at its start and 1/2 behind
+    dy, D = _np(gyt)[0], np.zeros((4, L))
+    for t in range(L - 1, -1, -1):
+        D[:, t] = dy[:, t] + (0.5 * D[:, t + 1] if t + 1 < L and (t + 1) % 3 else 0.0)
+    want = np.where(np.arange(L) % 3, 0.5, 1.0) * D
+    assert (np.abs(_np(gx)[0] - want) <= (16 * EPS + ref.HALF[dtype]) * (np.abs(want) + 4 * np.abs(dy).max())).all()
+    if dtype == "f32" and checkpoint is None:             # whatever lies in front of a stretch
+        x2 = xt.detach().clone()
+        x2[0, :, :3] = 1e30
+        x2.requires_grad_(True)
+        y2, _ = tnn.gated_scan(x2, gt, ht)
+        g2 = torch.autograd.grad(y2, (x2, gt), gyt)
+        assert torch.equal(y2[0, :, 3:], y[0, :, 3:]) and torch.equal(g2[0], gx) and torch.equal(g2[1][0, :, 3:], gg[0, :, 3:])
