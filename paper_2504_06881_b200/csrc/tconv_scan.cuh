@@ -88,16 +88,18 @@ struct Gate {
     Pair f, u;                       // 1 / (1 + e^-g) and 1 - f
 };
 // With z = e^-|g| = 2^-|g log2 e|, z / (1 + z) is the smaller of f and u and 1 / (1 + z) the larger: nothing overflows, and a gate
-// at an end of its type gives 0 and 1.  Subnormal z count as 0 (a gate beyond -+87.3 is fully shut or open); NaN passes.
+// at an end of its type gives 0 and 1.  Subnormal z count as 0 (a gate beyond -+87.3 is fully shut or open); NaN passes.  The larger
+// is formed as 1 less the smaller: 1 + z is rounded twice as coarsely as what lies below 1, and a gate that hardly decays has
+// every step of that come back over 1 / u positions.
 __device__ __forceinline__ Gate gate_of(Pair g) {
     const Pair t = mul2(g, {1.4426950408889634f, 1.4426950408889634f});
-    Pair z, large;
+    Pair z, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(z.lo) : "f"(-fabsf(t.lo)));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(z.hi) : "f"(-fabsf(t.hi)));
     const Pair d = add2(z, {1.0f, 1.0f});
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.lo) : "f"(d.lo));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.hi) : "f"(d.hi));
-    const Pair small = mul2(z, large);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.lo) : "f"(d.lo));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.hi) : "f"(d.hi));
+    const Pair small = mul2(z, r), large = fma2(small, {-1.0f, -1.0f}, {1.0f, 1.0f});
     const bool lo = g.lo < 0.0f, hi = g.hi < 0.0f;
     return {{lo ? small.lo : large.lo, hi ? small.hi : large.hi}, {lo ? large.lo : small.lo, hi ? large.hi : small.hi}};
 }

@@ -163,3 +163,47 @@ def test_scan_gradients_at_extreme_gates(L, checkpoint, dtype):
         y2, _ = tnn.gated_scan(x2, gt, ht)
         g2 = torch.autograd.grad(y2, (x2, gt), gyt)
         assert torch.equal(y2[0, :, 3:], y[0, :, 3:]) and torch.equal(g2[0], gx) and torch.equal(g2[1][0, :, 3:], gg[0, :, 3:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,L", [(1, 400001), (16, 8192), (200, 8192)])
+def test_scan_holds_a_constant(N, L, dtype):
+    """Constant candidates x from the state h0 = x under constant gates that hardly decay: h stays x but for roundings that come
+    back every step.  With f + u = 1 to half a step below 1, 2^-25 = EPS / 2, the fixed point u x / (1 - f) is off by EPS / 2u of x.
+    The decay of 256 positions is a product of 256 factors below 1: 255 roundings of EPS / 2 in whatever order, at worst all one way
+    since all are alike, EPS / 2u more; joining chunks and parts, and adding the state, take less than four roundings a chunk
+    (4 / 256 EPS / u).  Sums of candidates err by EPS of themselves ten times or so, and a position by some ten roundings of its own.
+    1.02 EPS / u + 20 EPS in all."""
+    gates = np.repeat(np.linspace(8.0, 13.5, 24)[None], N, 0)
+    g = _t(np.broadcast_to(gates[..., None], (N, 24, L)), dtype)
+    x = torch.full((N, 24, L), 0.7, dtype=DT[dtype], device="cuda")
+    h0 = x[..., 0].float()
+    y, last = tnn.gated_scan(x, g, h0)
+    u = 1 / (1 + np.exp(_np(g)[..., 0]))
+    off = 1.02 * EPS / u + 20 * EPS
+    err = np.abs(_np(last) / _np(h0) - 1)
+    assert (err <= off).all(), (err / off).max()
+    if dtype == "f32":
+        top = (y / h0[..., None] - 1).abs().amax(-1)
+        assert (_np(top) <= off + EPS).all(), (_np(top) / off).max()
+
+
+@pytest.mark.parametrize("L", [1, 9, 33, 129, 300])
+def test_scan_factors_add_up_to_one(L):
+    """f is what a state of one becomes with candidates of zero, u what candidates of one make of no state: the larger of the two
+    is 1 less the smaller, rounded once (EPS / 2), and the smaller within its own errors: e^-|g| to (|g| + 5) EPS, the sum, the
+    reciprocal (2 EPS) and the product to 4 EPS."""
+    g = np.concatenate([np.linspace(-80, 80, 4001), np.linspace(-14, 14, 20001), np.linspace(-0.1, 0.1, 2001)])
+    gt = torch.zeros(1, g.size, L, device="cuda")
+    gt[..., 0] = _t(g)
+    zero, one = torch.zeros_like(gt), torch.ones(1, g.size, device="cuda")
+    first = zero.clone()
+    first[..., 0] = 1
+    f, u = _np(tnn.gated_scan(zero, gt, one)[0])[0, :, 0], _np(tnn.gated_scan(first, gt)[0])[0, :, 0]
+    assert (np.abs(f + u - 1) <= EPS / 2).all()
+    gv = _np(gt)[0, :, 0]
+    e = np.exp(-np.abs(gv))
+    small, off = e / (1 + e), e / (1 + e) * (2 * np.abs(gv) + 9) * EPS
+    for got, less in ((f, gv < 0), (u, gv >= 0)):
+        want = np.where(less, small, 1 / (1 + e))
+        assert (np.abs(got - want) <= off + np.where(less, 0, EPS / 2)).all()
