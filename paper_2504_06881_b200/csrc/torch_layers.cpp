@@ -56,30 +56,30 @@ struct Desc {
 
 at::ScalarType type_of(const Geom& g) { return g.dtype == TCONV_F32 ? at::kFloat : at::kBFloat16; }
 
-Desc make_desc(const Geom& g, const Tensor& x, const Tensor& w) {
+Desc make_desc(const Geom& g, at::IntArrayRef x, const Tensor& w) {
     Desc d;
     const int nd = g.kind == kVolume ? 5 : 4;
-    TORCH_CHECK_VALUE(x.dim() == nd, "x: need a tensor of ", nd, " dimensions, got ", x.dim());
+    TORCH_CHECK_VALUE((int)x.size() == nd, "x: need a tensor of ", nd, " dimensions, got ", (int)x.size());
     const auto i = [](int64_t v) {
         TORCH_CHECK_VALUE(v <= INT32_MAX, "a size exceeds 31 bits");
         return (int32_t)v;
     };
     d.dims = nd;
     if (g.kind == kVolume) {
-        d.d3 = tconv3d_desc_t{i(x.size(0)), i(x.size(1)), i(x.size(2)), i(x.size(3)), i(x.size(4)), i(w.size(0)), i(w.size(2)),
+        d.d3 = tconv3d_desc_t{i(x[0]), i(x[1]), i(x[2]), i(x[3]), i(x[4]), i(w.size(0)), i(w.size(2)),
                               i(w.size(3)), i(w.size(4)), g.stride[0], g.stride[1], g.stride[2], g.pad[0], g.pad[1], g.pad[2],
                               g.dil[0], g.dil[1], g.dil[2], g.mode, g.chan, g.dtype};
         int32_t od, oh, ow;
         if (const int rc = tconv3d_output_shape(&d.d3, &od, &oh, &ow)) fail(rc, "tconv3d_output_shape");
-        d.y = {x.size(0), w.size(0), od, oh, ow};
+        d.y = {x[0], w.size(0), od, oh, ow};
     } else {
         const bool dw = g.kind == kDepthwise;
-        d.d2 = tconv_desc_t{i(x.size(0)), i(x.size(1)), i(x.size(2)), i(x.size(3)), i(dw ? x.size(1) : w.size(0)),
+        d.d2 = tconv_desc_t{i(x[0]), i(x[1]), i(x[2]), i(x[3]), i(dw ? x[1] : w.size(0)),
                             i(w.size(dw ? 1 : 2)), i(w.size(dw ? 2 : 3)), g.stride[0], g.stride[1], g.pad[0], g.pad[1],
                             g.dil[0], g.dil[1], g.mode, g.chan, g.dtype, TCONV_PAD_ZERO, TCONV_X_SAME};
         int32_t oh, ow;
         if (const int rc = tconv_output_shape(&d.d2, &oh, &ow)) fail(rc, "tconv_output_shape");
-        d.y = {x.size(0), d.d2.K, oh, ow, 0};
+        d.y = {x[0], d.d2.K, oh, ow, 0};
     }
     return d;
 }
@@ -114,7 +114,7 @@ struct Saved {
 Tensor run_forward(const Geom& g, const Tensor& x, const Tensor& w, const Tensor& w2, const Tensor& alpha, const Tensor& beta,
                    const Tensor& bias, bool want, Saved& s) {
     const auto dt = type_of(g);
-    const Desc d = make_desc(g, x, w);
+    const Desc d = make_desc(g, x.sizes(), w);
     TORCH_CHECK_VALUE(x.is_cuda(), "x: need a CUDA tensor, got one on ", x.device());
     c10::cuda::CUDAGuard guard(x.device());
     s.x = as(x, dt);
@@ -161,19 +161,21 @@ struct Grads {
     Tensor x, w, w2, alpha, beta, bias;
 };
 
-Grads run_backward(const Geom& g, const Saved& s, const Tensor& gy_in, bool need_x) {
-    const at::Device dev = s.x.device();
+// s.x undefined: no gradient of alpha or beta is wanted, and the input was of shape `shape`.
+Grads run_backward(const Geom& g, const Saved& s, at::IntArrayRef shape, const Tensor& gy_in, bool need_x) {
+    const bool have_x = s.x.defined();
+    const at::Device dev = (have_x ? s.x : s.w).device();
     const auto dt = type_of(g);
     const int wd = g.kind == kVolume ? 5 : g.kind == kDense ? 4 : 3;
-    TORCH_CHECK_VALUE(dev.is_cuda(), "x: need the CUDA tensor that the forward saved, got one on ", dev);
+    TORCH_CHECK_VALUE(dev.is_cuda(), have_x ? "x" : "w", ": need the CUDA tensor that the forward saved, got one on ", dev);
     TORCH_CHECK_VALUE(s.w.dim() == wd, "w: need the tensor of ", wd, " dimensions that the forward saved, got ", s.w.dim());
     c10::cuda::CUDAGuard guard(dev);
-    const Desc d = make_desc(g, s.x, s.w);
+    const Desc d = make_desc(g, shape, s.w);
     const Tensor gy = as(gy_in, dt);
     check_saved(gy, dev, dt, d.out(), "grad_y");
     const bool two = g.mode == TCONV_COMPOUND || g.mode == TCONV_PARALLEL, par = g.mode == TCONV_PARALLEL;
-    const auto opt = s.x.options(), f32 = opt.dtype(at::kFloat);
-    const int64_t K = d.y[1], C = s.x.size(1);
+    const auto opt = at::TensorOptions().device(dev).dtype(dt), f32 = opt.dtype(at::kFloat);
+    const int64_t K = d.y[1], C = shape[1];
     const int64_t kc[2] = {K, C};
     const at::IntArrayRef scalars = g.kind == kDepthwise ? at::IntArrayRef(kc, 1) : at::IntArrayRef(kc, 2);
     {
@@ -183,7 +185,7 @@ Grads run_backward(const Geom& g, const Saved& s, const Tensor& gy_in, bool need
         const int64_t wb[1] = {(int64_t)(g.kind == kVolume      ? tconv3d_winner_bytes(&d.d3)
                                          : g.kind == kDepthwise ? tconv_dw_winner_bytes(&d.d2)
                                                                 : tconv_winner_bytes(&d.d2))};
-        check_saved(s.x, dev, dt, s.x.sizes(), "x");
+        check_saved(s.x, dev, dt, shape, "x");
         check_saved(s.w, dev, dt, ws, "w");
         check_saved(s.w2, dev, dt, ws, "w2");
         check_saved(s.alpha, dev, at::kFloat, scalars, "alpha");
@@ -192,13 +194,19 @@ Grads run_backward(const Geom& g, const Saved& s, const Tensor& gy_in, bool need
         check_saved(s.winners, dev, at::kByte, wb, "winners");
     }
     Grads r;
-    if (need_x || g.kind == kDepthwise) r.x = at::empty(s.x.sizes(), opt);
+    if (need_x || g.kind == kDepthwise) r.x = at::empty(shape, opt);
     r.w = at::empty(s.w.sizes(), f32);
     if (par) r.w2 = at::empty(s.w.sizes(), f32);
-    if (two) {
+    if (two && have_x) {
         r.alpha = at::empty(scalars, f32);
         r.beta = at::empty(scalars, f32);
     }
+    // What stands in for an x that was not kept.  The kernels read x for grad_alpha and grad_beta alone, and not at all where those
+    // are not asked for, but for the three-dimensional ones with two branches, which sum them all the same: they get grad_x, which
+    // is written before they run, or a tensor of that size.
+    Tensor instead;
+    if (!have_x) instead = !(two && g.kind == kVolume) ? gy : r.x.defined() ? r.x : at::empty(shape, opt);
+    const void* px = ptr(have_x ? s.x : instead);
     r.bias = at::empty({K}, f32);
     const auto scratch = [&](size_t n) { return n ? at::empty({(int64_t)n}, opt.dtype(at::kByte)) : Tensor(); };
     int rc;
@@ -207,13 +215,13 @@ Grads run_backward(const Geom& g, const Saved& s, const Tensor& gy_in, bool need
         const size_t n = tconv3d_workspace_bytes(&d.d3, 1);
         const Tensor ws = scratch(n);
         where = "tconv3d_backward";
-        rc = tconv3d_backward(&d.d3, ptr(s.x), ptr(s.w), ptr(s.w2), fptr(s.alpha), fptr(s.beta), ptr(gy), ptr(s.winners), ptr(r.x),
+        rc = tconv3d_backward(&d.d3, px, ptr(s.w), ptr(s.w2), fptr(s.alpha), fptr(s.beta), ptr(gy), ptr(s.winners), ptr(r.x),
                               fptr(r.w), fptr(r.w2), fptr(r.alpha), fptr(r.beta), fptr(r.bias), ptr(ws), n, stream());
     } else if (g.kind == kDepthwise) {
         const size_t n = tconv_dw_workspace_bytes(&d.d2, 1);
         const Tensor ws = scratch(n);
         where = "tconv_dw_backward";
-        rc = tconv_dw_backward(&d.d2, ptr(s.x), ptr(s.w), ptr(s.w2), fptr(s.alpha), fptr(s.beta), ptr(gy), ptr(s.winners), ptr(r.x),
+        rc = tconv_dw_backward(&d.d2, px, ptr(s.w), ptr(s.w2), fptr(s.alpha), fptr(s.beta), ptr(gy), ptr(s.winners), ptr(r.x),
                                fptr(r.w), fptr(r.w2), fptr(r.alpha), fptr(r.beta), fptr(r.bias), ptr(ws), n, stream());
     } else {
         // the figure includes room for recomputed winners, which are passed here
@@ -222,7 +230,7 @@ Grads run_backward(const Geom& g, const Saved& s, const Tensor& gy_in, bool need
         n = n > kept ? n - kept : 0;
         const Tensor ws = scratch(n);
         where = "tconv_backward";
-        rc = tconv_backward(&d.d2, ptr(s.x), ptr(s.w), ptr(s.w2), fptr(s.alpha), fptr(s.beta), ptr(gy), ptr(s.winners), ptr(r.x),
+        rc = tconv_backward(&d.d2, px, ptr(s.w), ptr(s.w2), fptr(s.alpha), fptr(s.beta), ptr(gy), ptr(s.winners), ptr(r.x),
                             fptr(r.w), fptr(r.w2), fptr(r.alpha), fptr(r.beta), fptr(r.bias), ptr(ws), n, stream());
     }
     if (rc) fail(rc, where);
@@ -244,17 +252,20 @@ public:
                                                        g.pad[0], g.pad[1], g.pad[2], g.dil[0], g.dil[1], g.dil[2]};
         ctx->saved_data["given"] = (int64_t)((w2.defined() ? 1 : 0) | (alpha.defined() ? 2 : 0) | (beta.defined() ? 4 : 0) |
                                              (bias.defined() ? 8 : 0));
-        if (q8) {       // x in 8 bits, as the caller has it or stored here
+        if (q8) {       // x in 8 bits, as the caller has it or stored here; nothing of it where alpha and beta learn nothing
             const auto [rows, inner] = tconv_torch::q8_rows(x.sizes());
             c10::cuda::CUDAGuard guard(x.device());
             tconv_torch::Q8 q{given(codes_), given(scales_)};
-            if (q.codes.defined()) {
-                tconv_torch::q8_check(q, x, rows, inner);
-            } else {
+            if (q.codes.defined()) tconv_torch::q8_check(q, x, rows, inner);
+            const bool two = g.mode == TCONV_COMPOUND || g.mode == TCONV_PARALLEL;
+            if (!(two && ((alpha.defined() && alpha.requires_grad()) || (beta.defined() && beta.requires_grad())))) {
+                q = {};
+            } else if (!q.codes.defined()) {
                 q = tconv_torch::q8_empty(x, rows, inner);
                 if (const int rc = tconv_q8_store(rows, inner, g.dtype, ptr(s.x), ptr(q.codes), ptr(q.scales), stream())) fail(rc, "tconv_q8_store");
             }
             ctx->saved_data["x"] = x.sizes().vec();
+            ctx->saved_data["kept"] = q.codes.defined();
             ctx->save_for_backward({q.codes, s.w, s.w2, s.alpha, s.beta, s.winners, q.scales});
         } else {
             ctx->save_for_backward({s.x, s.w, s.w2, s.alpha, s.beta, s.winners});
@@ -269,8 +280,9 @@ public:
         const Geom g{n(0), n(1), n(2), n(3), {n(4), n(5), n(6)}, {n(7), n(8), n(9)}, {n(10), n(11), n(12)}};
         const int64_t has = ctx->saved_data["given"].toInt();
         if (!gys[0].defined()) return variable_list(10);
-        if (v.size() == 7) {
-            const auto shape = ctx->saved_data["x"].toIntVector();
+        std::vector<int64_t> shape;
+        if (v.size() == 7) shape = ctx->saved_data["x"].toIntVector();
+        if (v.size() == 7 && ctx->saved_data["kept"].toBool()) {
             const auto [rows, inner] = tconv_torch::q8_rows(shape);
             TORCH_CHECK_VALUE(v[0].defined() && v[0].is_cuda() && v[6].defined(), "codes, scales: need the CUDA tensors that the forward saved");
             tconv_torch::q8_check({v[0], v[6]}, v[0], rows, inner);
@@ -278,7 +290,7 @@ public:
             s.x = at::empty(shape, v[0].options().dtype(type_of(g)));
             if (const int rc = tconv_q8_restore(rows, inner, g.dtype, ptr(v[0]), ptr(v[6]), ptr(s.x), stream())) fail(rc, "tconv_q8_restore");
         }
-        Grads r = run_backward(g, s, gys[0], ctx->needs_input_grad(0));
+        Grads r = run_backward(g, s, v.size() == 7 ? at::IntArrayRef(shape) : s.x.sizes(), gys[0], ctx->needs_input_grad(0));
         const auto in_type = (at::ScalarType)ctx->saved_data["in_type"].toInt();
         if (r.x.defined() && r.x.scalar_type() != in_type) r.x = r.x.to(in_type);
         const auto if_given = [&](const Tensor& t, int bit) { return (has & bit) ? t : Tensor(); };

@@ -276,7 +276,8 @@ class TropicalConv2d(nn.Module):
     ``fixed=(alpha, beta)``, e.g. (0.5, 0.5) or (1, -1), held as buffers.
     dtype: arithmetic type of the kernels ("f32" or "bf16"); parameters stay fp32.
     checkpoint="q8": the backward pass keeps the input in 8 bits (see Q8) in place of the tensor itself.  It is read for
-    the gradients of alpha and beta alone, which are then those over the restored input; all others are the same.
+    the gradients of alpha and beta alone, which are then those over the restored input; all others are the same.  Where
+    neither learns (max_plus, min_plus, "0p", "fixed", frozen scalars) nothing of the input is kept.
     forward's `stored` is the input's Q8 where it is there already (rms_norm's second output)."""
 
     PARAMS = ("0p", "1p", "2p", "shared", "opposite", "fixed")
