@@ -318,7 +318,8 @@ int tconv_scan_backward(const tconv_scan_desc_t *desc, const void *x, const void
  * place.  Backward, with z = s * rstd:
  *     grad_x = rstd * (weight * grad_y - z * mean_c(weight * grad_y * z)) + grad_sum  (grad_sum NULL: 0),
  * which is the gradient of the residual too, and grad_weight[c] = sum of grad_y * z (NULL: not wanted);
- * s is NULL where s_codes and s_scales are given.  Dense tensors; fixed order of every sum, no atomics.
+ * s is NULL where s_codes and s_scales are given.  Dense tensors; fixed order of every sum, no atomics.  N and C are
+ * 2^31 - 4096 at most.
  */
 typedef struct {
     int32_t N, C;

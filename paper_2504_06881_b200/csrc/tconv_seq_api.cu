@@ -125,6 +125,8 @@ int check_norm(const tconv_norm_desc_t* d, NormArgs* a) {
     if (!d || d->N <= 0 || d->C <= 0 || d->P <= 0 || (d->dtype != TCONV_F32 && d->dtype != TCONV_BF16) || !(d->eps >= 0))
         return TCONV_ERR_INVALID_ARG;
     if ((int64_t)d->N * d->C > kMost / d->P || (int64_t)d->N > (int64_t)INT32_MAX / q8_blocks(d->P)) return TCONV_ERR_TOO_LARGE;
+    // (channels and rows are counted in 32 bits, up to a thousand beyond the last among them)
+    if (d->N > INT32_MAX - 4095 || d->C > INT32_MAX - 4095) return TCONV_ERR_TOO_LARGE;
     *a = NormArgs{d->N, d->C, d->P, d->eps};
     return TCONV_OK;
 }
