@@ -429,8 +429,11 @@ public:
         }
         same(go[0], v[0], type, shape, "grad_y");
         same(gsum, v[0], type, shape, "grad_sum");
-        const Tensor kept = dense(v[0]), w = dense(v[1]), gs = dense(gsum);
-        const Tensor gy = go[0].defined() ? dense(go[0]) : at::zeros(shape, kept.options().dtype(type));
+        if (!go[0].defined()) {       // the stream's gradient is passed on, whatever the stream holds
+            const Tensor gx = gsum.contiguous();
+            return {gx, ctx->needs_input_grad(1) ? at::zeros(c, v[1].options()) : Tensor(), gx, Tensor(), Tensor(), Tensor()};
+        }
+        const Tensor kept = dense(v[0]), w = dense(v[1]), gs = dense(gsum), gy = dense(go[0]);
         Tensor gx = fresh(shape, type, kept), gw;
         if (ctx->needs_input_grad(1)) gw = fresh(c, at::kFloat, kept);
         const size_t n = gw.defined() ? tconv_norm_workspace_bytes(&d) : 0;

@@ -207,3 +207,28 @@ def test_scan_factors_add_up_to_one(L):
     for got, less in ((f, gv < 0), (u, gv >= 0)):
         want = np.where(less, small, 1 / (1 + e))
         assert (np.abs(got - want) <= off + np.where(less, 0, EPS / 2)).all()
+
+
+# ---- gradients of one output, and the step -------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("checkpoint", [None, "q8"])
+@pytest.mark.parametrize("shape", [(2, 40), (2, 33, 50), (2, 1030, 40)])
+def test_norm_stream_alone_passes_its_gradient_on(shape, checkpoint, dtype):
+    """Where only the stream is used its gradient is that of x and of the residual, whatever the stream holds; the weight's is 0."""
+    rs = np.random.RandomState(1)
+    x, r = _t(rs.standard_normal(shape), dtype), _t(rs.standard_normal(shape), dtype)
+    x.view(-1)[3], x.view(-1)[77] = float("inf"), float("nan")
+    w, up = torch.ones(shape[1], device="cuda", requires_grad=True), _t(rs.standard_normal(shape), dtype)
+    x.requires_grad_(True)
+    r.requires_grad_(True)
+    s = tnn.rms_norm(x, w, r, checkpoint=checkpoint).stream
+    gx, gw, gr = torch.autograd.grad(s, (x, w, r), up, retain_graph=True)
+    assert torch.equal(gx, up) and torch.equal(gr, up) and (gw == 0).all() and gw.shape == w.shape
+    (gx,) = torch.autograd.grad(s, (x,), up.transpose(0, 1).contiguous().transpose(0, 1))      # strided, and one wanted alone
+    assert torch.equal(gx, up)
+    # leaves have gradients of their own: not the caller's tensor, nor each other's
+    tnn.rms_norm(x, w, r, checkpoint=checkpoint).stream.backward(up)
+    assert torch.equal(x.grad, up) and torch.equal(r.grad, up) and (w.grad == 0).all()
+    before = up.clone()
+    x.grad.add_(1)
+    assert torch.equal(r.grad, before) and torch.equal(up, before)
