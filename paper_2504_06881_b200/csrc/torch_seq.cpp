@@ -309,9 +309,21 @@ std::tuple<Tensor, Tensor> gated_scan_step(const Tensor& h, const Tensor& x, con
     if (out.defined()) {
         same(out, x, at::kFloat, nc, "out");
         TORCH_CHECK_VALUE(out.is_contiguous() && !(reinterpret_cast<uintptr_t>(out.data_ptr()) & 15), "out: need a contiguous tensor aligned to 16 bytes");
-        const auto lo = [](const Tensor& t) { return (const char*)t.data_ptr(); };
-        const auto hi = [&](const Tensor& t) { return lo(t) + t.nbytes(); };
-        TORCH_CHECK_VALUE(lo(out) == lo(h0) || hi(out) <= lo(h0) || hi(h0) <= lo(out), "out: overlaps h without being it");
+        const char *lo = (const char*)out.data_ptr(), *hi = lo + out.nbytes();
+        const auto meets = [&](const void* p, int64_t bytes) { return lo < (const char*)p + bytes && (const char*)p < hi; };
+        TORCH_CHECK_VALUE(ptr(h0) == lo || !meets(ptr(h0), h0.nbytes()), "out: overlaps h without being it");
+        // an input that lies just like out is read before out is written; another one must not share memory with it
+        const auto apart = [&](const void* p, int64_t batch, int64_t row, int64_t es) {
+            if (p == lo && es == 4 && (s.d.N == 1 || batch == s.d.C) && (s.d.C == 1 || row == 1)) return true;
+            const int64_t width = ((s.d.C - 1) * row + 1) * es;
+            if (!meets(p, (s.d.N - 1) * batch * es + width)) return true;
+            for (int64_t n = 0; n < s.d.N; ++n)
+                if (meets((const char*)p + n * batch * es, width)) return false;
+            return true;
+        };
+        const int64_t es = s.x.element_size();
+        TORCH_CHECK_VALUE(apart(s.px, s.d.x_batch, s.d.x_row, es), "out: overlaps x");
+        TORCH_CHECK_VALUE(apart(s.pg, s.d.gate_batch, s.d.gate_row, es), s.packed ? "out: overlaps x" : "out: overlaps gate");
         last = out;
     } else {
         last = fresh(nc, at::kFloat, h0);

@@ -614,7 +614,8 @@ def gated_scan(x, gate=None, h0=None, lengths=None, checkpoint=None):
 
 def gated_scan_step(h, x, gate=None, out=None):
     """One position of gated_scan for streaming: state h float32 [N, C], x and gate [N, C] (or x [N, 2C] alone).
-    Returns y and the new state, written to `out` if given, which may be h.  Records no gradients."""
+    Returns y and the new state, written to `out` if given, which may be h and shares no memory with x or gate.  Records
+    no gradients."""
     return _native.gated_scan_step(h, x, gate, out)
 
 

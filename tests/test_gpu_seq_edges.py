@@ -232,3 +232,26 @@ def test_norm_stream_alone_passes_its_gradient_on(shape, checkpoint, dtype):
     before = up.clone()
     x.grad.add_(1)
     assert torch.equal(r.grad, before) and torch.equal(up, before)
+
+
+def test_step_refuses_a_state_that_overlaps_its_inputs():
+    buf = torch.randn(64, device="cuda")
+    h, x, g = torch.randn(2, 8, device="cuda"), torch.randn(2, 8, device="cuda"), torch.randn(2, 8, device="cuda")
+    with torch.no_grad():
+        want, state = tnn.gated_scan_step(h, x, g)
+        for call in (lambda: tnn.gated_scan_step(h, buf[:16].view(2, 8), g, out=buf[4:20].view(2, 8)),
+                     lambda: tnn.gated_scan_step(h, x, buf[16:32].view(2, 8), out=buf[4:20].view(2, 8)),
+                     lambda: tnn.gated_scan_step(h, buf[:32].view(2, 16), out=buf[28:44].view(2, 8)),
+                     lambda: tnn.gated_scan_step(h, buf[:64].view(8, 8)[::4], g, out=buf[24:40].view(2, 8))):
+            with pytest.raises(ValueError, match="overlaps"):
+                call()
+        # neighbours are fine: next to each other, between the rows of a wider tensor; and the state itself
+        buf.view(8, 8)[::4].copy_(x)
+        y, out = tnn.gated_scan_step(h, buf.view(8, 8)[::4], g, out=buf[12:28].view(2, 8))
+        assert torch.equal(y, want) and torch.equal(out, state) and torch.equal(buf.view(8, 8)[::4], x)
+        buf[:16].copy_(x.view(-1))
+        buf[16:32].copy_(g.view(-1))
+        y, out = tnn.gated_scan_step(h, buf[:16].view(2, 8), buf[16:32].view(2, 8), out=buf[32:48].view(2, 8))
+        assert torch.equal(y, want) and torch.equal(out, state)
+        y, out = tnn.gated_scan_step(h, x, g, out=h)
+        assert torch.equal(y, want) and torch.equal(out, state)
