@@ -112,6 +112,7 @@ using tconv_torch::q8_rows;
 
 std::tuple<Tensor, Tensor> q8_store(const Tensor& x) {
     no_trace("q8_store");
+    no_tangent(x, "q8_store");
     const int dt = dtype_of(x, "x");
     c10::cuda::CUDAGuard guard(x.device());
     const auto [rows, inner] = q8_rows(x.sizes());
@@ -295,6 +296,7 @@ std::tuple<Tensor, Tensor> gated_scan(const Tensor& x, const OptTensor& gate_, c
 std::tuple<Tensor, Tensor> gated_scan_step(const Tensor& h, const Tensor& x, const OptTensor& gate_, const OptTensor& out_) {
     no_trace("gated_scan_step");
     const Tensor gate = given(gate_), out = given(out_);
+    for (const Tensor* t : {&h, &x, &gate}) no_tangent(*t, "gated_scan_step");
     TORCH_CHECK_VALUE(!records({&h, &x, &gate, &out}), "gated_scan_step: records no gradients; use gated_scan, or call it under torch.no_grad()");
     TORCH_CHECK_VALUE(x.is_cuda(), "x: need a CUDA tensor, got one on ", x.device());
     TORCH_CHECK_VALUE(x.dim() == 2, "x: need a tensor of 2 dimensions, got ", x.dim());

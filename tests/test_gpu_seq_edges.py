@@ -255,3 +255,37 @@ def test_step_refuses_a_state_that_overlaps_its_inputs():
         assert torch.equal(y, want) and torch.equal(out, state)
         y, out = tnn.gated_scan_step(h, x, g, out=h)
         assert torch.equal(y, want) and torch.equal(out, state)
+
+
+def test_step_and_store_refuse_tangents():
+    import torch.autograd.forward_ad as fwad
+    h, x, g = (torch.randn(2, 8, device="cuda") for _ in range(3))
+    for k in range(3):
+        with torch.no_grad(), fwad.dual_level(), pytest.raises(NotImplementedError, match="forward-mode"):
+            t = [h, x, g]
+            t[k] = fwad.make_dual(t[k], torch.ones_like(t[k]))
+            tnn.gated_scan_step(*t)
+    with fwad.dual_level(), pytest.raises(NotImplementedError, match="forward-mode"):
+        tnn.q8_store(fwad.make_dual(x, torch.ones_like(x)))
+
+
+@pytest.mark.parametrize("checkpoint", [None, "q8"])
+def test_function_transforms_are_refused(checkpoint):
+    """As the layers': what a transform hands over has no memory of its own."""
+    x, g, h = torch.randn(2, 4, 8, device="cuda"), torch.randn(2, 4, 8, device="cuda"), torch.randn(2, 4, device="cuda")
+    w, many = torch.ones(4, device="cuda"), lambda t: torch.stack([t, t])
+    calls = [(lambda v: tnn.gated_scan(v, g, checkpoint=checkpoint)[0], x), (lambda v: tnn.gated_scan(x, v, checkpoint=checkpoint)[0], g),
+             (lambda v: tnn.gated_scan(x, g, v, checkpoint=checkpoint)[0], h),
+             (lambda v: tnn.rms_norm(v, w, checkpoint=checkpoint).y, x), (lambda v: tnn.rms_norm(x, v, checkpoint=checkpoint).y, w),
+             (lambda v: tnn.rms_norm(x, w, v, checkpoint=checkpoint).y, x)]
+    for fn, t in calls:
+        for record in (True, False):
+            with torch.set_grad_enabled(record), pytest.raises(RuntimeError):
+                torch.func.vmap(fn)(many(t))
+        with pytest.raises(RuntimeError):
+            torch.func.grad(lambda v: fn(v).sum())(t)
+    for fn, t in ((lambda v: tnn.q8_store(v).restore(), x), (lambda v: tnn.gated_scan_step(v, x[..., 0], g[..., 0])[0], h),
+                  (lambda v: tnn.gated_scan_step(h, v, g[..., 0])[0], h),
+                  (lambda v: tnn.gated_scan(x, g, lengths=v)[0], torch.tensor([3, 8], dtype=torch.int32, device="cuda"))):
+        with pytest.raises(RuntimeError), torch.no_grad():
+            torch.func.vmap(fn)(many(t))
