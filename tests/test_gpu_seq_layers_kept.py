@@ -3,7 +3,7 @@ convolution is handed."""
 import pytest
 import torch
 
-from paper_2504_06881_b200 import layers as tlayers, nn as tnn, tconv, tconv3d
+from paper_2504_06881_b200 import inputs, layers as tlayers, nn as tnn, tconv, tconv3d
 
 pytestmark = pytest.mark.gpu
 
@@ -115,3 +115,56 @@ def test_backward_holds_no_copy_of_an_input_it_does_not_read():
         peaks.append(torch.cuda.max_memory_allocated() - held)
         del y, up, g
     assert peaks[1] <= peaks[0] + 4096
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("first", [True, False])
+def test_block_with_kept_activations(first, dtype):
+    """The recurrent block with checkpoint="q8" is its parts, the convolution's input kept as the norm's own 8-bit output (of y in
+    fp32, before the convolution's rounding): every gradient bit for bit, those of alpha and beta over that form's values.
+
+    Against the block that keeps everything: a restored value is off by 1/127 of its block's largest at most, some 0.05 for normalised
+    signals whose largest is 6.  f (1 - f) moves by as much relatively, f's products over the 1 / (1 - f) positions that a state
+    lasts by as much again, h - x and a branch value by 0.05 each; with the norm's stream, a quarter of a gradient's norm at most."""
+    torch.manual_seed(5)
+    blocks = [tlayers.TropicalRecurrentBlock1d(16, dtype=dtype, checkpoint=ck).cuda() for ck in ("q8", None)]
+    with torch.no_grad():
+        for n, p in blocks[0].named_parameters():
+            p.mul_(torch.empty_like(p).uniform_(0.5, 1.5))
+    blocks[1].load_state_dict(blocks[0].state_dict())
+    block = blocks[0]
+    x = torch.randn(2, 16, 333, device="cuda", requires_grad=True)
+    r = None if first else torch.randn(2, 16, 333, device="cuda", requires_grad=True)
+    lengths = torch.tensor([333, 200], dtype=torch.int32, device="cuda")
+    ups = [torch.randn_like(x)] + [torch.randn_like(x)] * (not first)
+
+    def grads(of, block):
+        y, stream = of(block)
+        ins = [x] + [r] * (not first) + list(block.parameters())
+        return (y, stream) + torch.autograd.grad([y] + [stream] * (not first), ins, ups)
+
+    inner = block.rec.conv.conv                           # the 1 x 3 windows of the signal's layer
+    seen = {}
+
+    def by_hand(b):
+        n = tnn.rms_norm(x, b.norm.weight, r, b.norm.eps, "both", "q8")
+        both = inner(n.y.unsqueeze(2), n.q8).squeeze(2)
+        both.register_hook(lambda g: seen.update(grad=g.detach().clone()))
+        seen.update(n=n)
+        return tnn.gated_scan(both, None, None, lengths, "q8")[0], n.stream
+
+    got = grads(lambda b: b(x, r, lengths), block)
+    hand = grads(by_hand, block)
+    assert len(got) == len(hand) and all(torch.equal(a, b) for a, b in zip(got, hand))
+    dt = tconv.TORCH_DTYPE[dtype]
+    d = inputs.layer(2, 16, 1, 333, 32, 1, 3, pad=(0, 1), mode="compound", dtype=dtype)
+    xc, w = seen["n"].y.detach().to(dt).unsqueeze(2), inner.weight.detach().to(dt)
+    a, b = inner.alpha.detach(), inner.beta.detach()
+    _, winners = tconv.forward(d, xc, w, None, a, b, inner.bias.detach(), want_winners=True)
+    want = tconv.backward(d, seen["n"].q8.restore(dt).unsqueeze(2), w, seen["grad"].to(dt).unsqueeze(2), None, a, b, winners)
+    named = dict(zip([n for n, _ in block.named_parameters()], got[-len(list(block.parameters())):]))
+    assert torch.equal(named["rec.conv.conv.alpha"], want["grad_alpha"]) and torch.equal(named["rec.conv.conv.beta"], want["grad_beta"])
+    full = grads(lambda b: b(x, r, lengths), blocks[1])
+    assert torch.equal(got[0], full[0]) and torch.equal(got[1], full[1])
+    for k, (u, v) in enumerate(zip(got[2:], full[2:])):
+        assert v.norm() > 0 and (u - v).norm() <= 0.25 * v.norm(), k
