@@ -771,7 +771,7 @@ scan_bwd_kernel(const __grid_constant__ ScanArgs a,
             for (int i = 3; i >= 0; --i) {
                 const Pair D = add2({d[i], d[i + 4]}, w);
                 w = mul2(f[i], D);
-                const Pair dx = mul2(u[i], D), dg = mul2(mul2(w, b[i]), u[i]);
+                const Pair dx = mul2(u[i], D), dg = mul2(mul2(w, u[i]), b[i]);
                 x[i] = WHOLE || i < live ? dx.lo : 0.0f;
                 x[i + 4] = WHOLE || i + 4 < live ? dx.hi : 0.0f;
                 g[i] = WHOLE || i < live ? dg.lo : 0.0f;

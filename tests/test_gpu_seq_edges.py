@@ -289,3 +289,29 @@ def test_function_transforms_are_refused(checkpoint):
                   (lambda v: tnn.gated_scan(x, g, lengths=v)[0], torch.tensor([3, 8], dtype=torch.int32, device="cuda"))):
         with pytest.raises(RuntimeError), torch.no_grad():
             torch.func.vmap(fn)(many(t))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("checkpoint", [None, "q8"])
+@pytest.mark.parametrize("L", LENGTHS)
+def test_scan_skips_lowest_values_behind_open_gates(L, checkpoint, dtype):
+    """Positions masked by the type's lowest value and a fully open gate: the state passes them, they have no gradients, and all
+    others are what they are with zeros there, bit for bit, under upstream gradients of any size."""
+    most = float(torch.finfo(DT[dtype]).max)
+    rs = np.random.RandomState(L)
+    masked = torch.from_numpy(rs.rand(2, 5, L) < 0.3).cuda()
+    masked[..., 0] = True
+    x, g = _t(rs.standard_normal((2, 5, L)), dtype), _t(rs.standard_normal((2, 5, L)), dtype)
+    h0, gy, gh = _t(rs.standard_normal((2, 5)), grad=True), _t(100 * rs.standard_normal((2, 5, L)), dtype), _t(rs.standard_normal((2, 5)))
+    if checkpoint:                                        # whole rows of masks, alone in their 8-bit blocks
+        masked[:] = False
+        masked[1] = True
+    g[masked] = most
+    runs = []
+    for value in (0.0, -most):
+        xi, gi = torch.where(masked, value, x).to(DT[dtype]).requires_grad_(True), g.detach().requires_grad_(True)
+        y, last = tnn.gated_scan(xi, gi, h0, checkpoint=checkpoint)
+        runs.append((y, last) + torch.autograd.grad((y, last), (xi, gi, h0), (gy, gh)))
+        assert all(torch.isfinite(t).all() for t in runs[-1])
+        assert (runs[-1][2][masked] == 0).all() and (runs[-1][3][masked] == 0).all()
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
