@@ -313,6 +313,8 @@ int tconv_scan_backward(const tconv_scan_desc_t *desc, const void *x, const void
  * Root-mean-square norm over the channels of [N][C][P] (P = 1: rows of C values), with the residual's addition:
  *     s = x + residual, rounded to the tensors' type (residual NULL: s = x, and `sum` is not written);
  *     rstd = 1 / sqrt(mean_c(s^2) + eps);   y = s * rstd * weight[c].
+ * Squares are summed in fp32: where finite values (from some 1.8e19 on) take a position's sum beyond it rstd is 0, and so
+ * are y and the gradient through the norm.
  * y may be NULL where its 8-bit form (y_codes, y_scales) is wanted alone.  rstd (fp32 [N][P], NULL: not wanted)
  * and s are what a backward pass needs; s_codes and s_scales, if given, take the 8-bit form of s to be kept in its
  * place.  Backward, with z = s * rstd:

@@ -800,8 +800,9 @@ struct NormPlan {
 };
 
 // The kernels with P > 1, by values at a time, warps, and channels of a thread, from the smallest that holds all channels on.  The
-// last one by single values is at the limit of its registers, and still ahead of the kernel in groups where maps are small (64 x 512 x
-// 7 x 7 bf16 forward 7.7 us against 11.6) and even with it where they are large (8 x 512 x 8191 bf16 forward and backward 102 + 206
+// last one by single values is at the limit of its registers (its backward from a stream in 8 bits beyond: of a word a code 336 to
+// 432 bytes a thread go to local memory, 64 x 512 x 7 x 7 bf16 32 us), and still ahead of the kernel in groups where maps are small
+// (64 x 512 x 7 x 7 bf16 forward 7.7 us against 11.6) and even with it where they are large (8 x 512 x 8191 bf16 forward and backward 102 + 206
 // against 133 + 183).  Four bf16 values at a time against single ones: 86 + 82 us for 7 x 494 x 13044 (the whole pass 222 against 642).
 template <typename F> void with_cols(std::integral_constant<int, 8>, int form, F f) {
     if (form == 0) f.template operator()<8, 4, 2>();

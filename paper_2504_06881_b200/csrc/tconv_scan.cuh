@@ -6,8 +6,8 @@
 // state.  Rows go to warps; where there are fewer rows than keep the GPU busy, a block's warps take a row's chunks in turn and
 // hand the state round, and where there are very few a first kernel joins the maps of parts of a row.
 // HBM is the bound (6 bytes a position forward in bf16, 10 backward) where rows start on 16 bytes: 64 x 256 x 8192 bf16, half of
-// it live, takes 87 and 156 us, 5.8 TB/s.  At 29 and 50 instructions a position the issue slots and, for odd 16-bit rows, the
-// shared-memory path are nearly as short (32 x 128 x 3981: 29 and 40 us, 3.4 and 4.1 TB/s), so that whatever is not arithmetic
+// it live, takes 88 and 157 us, 5.8 TB/s.  At 31 and 52 instructions a position the issue slots and, for odd 16-bit rows, the
+// shared-memory path are nearly as short (32 x 128 x 3981: 29 and 40 us, 3.3 and 4.1 TB/s), so that whatever is not arithmetic
 // is kept out of the whole chunks' way.
 #pragma once
 #include "tconv_q8.cuh"
@@ -90,7 +90,10 @@ struct Gate {
 // With z = e^-|g| = 2^-|g log2 e|, z / (1 + z) is the smaller of f and u and 1 / (1 + z) the larger: nothing overflows, and a gate
 // at an end of its type gives 0 and 1.  Subnormal z count as 0 (a gate beyond -+87.3 is fully shut or open); NaN passes.  The larger
 // is formed as 1 less the smaller: 1 + z is rounded twice as coarsely as what lies below 1, and a gate that hardly decays has
-// every step of that come back over 1 / u positions.
+// every step of that come back over 1 / u positions.  Against 1 / (1 + e^-g) with e^-g held to 2^115, and u = e^-g f, this costs two
+// to three instructions a gate: nothing where memory bounds, 33 -> 37 us forward where there are two gates a position and half the
+// bytes (32 x 128 x 4000 bf16 kept in 8 bits).  By a sign on z and packed sums in place of the selects 36 us there, but 18 for 16
+// in parts of a long row; by a Newton step on both packed sides 164 us for 157 backward in 64 x 256 x 8192.
 __device__ __forceinline__ Gate gate_of(Pair g) {
     const Pair t = mul2(g, {1.4426950408889634f, 1.4426950408889634f});
     Pair z, r;
@@ -813,7 +816,7 @@ scan_bwd_kernel(const __grid_constant__ ScanArgs a,
 
 // How a row's positions are shared out: short rows several to a warp; a row to a warp where there are rows enough; a block's warps
 // in turn on a row, up to eight, in one pass; below that parts of a row, a warp each, in two passes (24 rows of 400001 positions:
-// 27 us against 52 with the parts in blocks whose warps take turns).
+// 28 us against 52 with the parts in blocks whose warps take turns).
 struct ScanPlan {
     int g, warps, parts;             // threads of a row (1, 4, 16, 32); warps of a block on one row; parts of a row, a warp each
     uint32_t per_part;               // chunks

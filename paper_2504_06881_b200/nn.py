@@ -684,7 +684,8 @@ class TropicalRecurrentBlock1d(nn.Module):
     """Residual block of a network over long signals: RMS norm of the stream, tropical recurrence, and its output's addition
     left to the next block's norm.  forward(x, residual=None) gives the branch and the stream, which the next block
     (or a last RMSNorm) takes as its x and residual; the first block takes its input as x.  checkpoint="q8": the stream,
-    the convolution's input (in the norm's own 8-bit output) and the recurrence's are kept in 8 bits."""
+    the convolution's input (as the norm's own 8-bit output, of y before it is rounded to x's type or the layer's) and the
+    recurrence's are kept in 8 bits."""
 
     def __init__(self, channels, kernel_size=3, padding=1, mode="compound", params="2p", dtype="f32", eps=1e-6,
                  checkpoint=None):
