@@ -315,3 +315,33 @@ def test_scan_skips_lowest_values_behind_open_gates(L, checkpoint, dtype):
         assert all(torch.isfinite(t).all() for t in runs[-1])
         assert (runs[-1][2][masked] == 0).all() and (runs[-1][3][masked] == 0).all()
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("checkpoint", [None, "q8"])
+@pytest.mark.parametrize("shape", [(2, 40), (2, 1028), (2, 40, 33), (2, 40, 64), (1, 520, 40)])
+def test_norm_of_sums_beyond_fp32(shape, checkpoint, dtype):
+    """A position whose squares leave fp32: y is 0 there, the gradient through the norm as well, and other positions are what they are;
+    where a position lies in its neighbours' 8-bit blocks, theirs are not compared."""
+    most = float(torch.finfo(DT[dtype]).max)
+    gen = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn(shape, device="cuda", generator=gen).to(DT[dtype])
+    gy, gs = torch.randn(shape, device="cuda", generator=gen).to(DT[dtype]), torch.randn(shape, device="cuda", generator=gen).to(DT[dtype])
+    r, w = torch.zeros_like(x), torch.ones(shape[1], device="cuda")
+
+    def run(x):
+        x = x.clone().requires_grad_(True)
+        o = tnn.rms_norm(x, w, r, checkpoint=checkpoint)
+        return (o.y.detach(),) + torch.autograd.grad((o.y, o.stream), x, (gy, gs))
+
+    clean = run(x)
+    at = (0, slice(None)) + (5,) * (len(shape) - 2)
+    x[at][::2] = -most
+    y, gx = run(x)
+    assert (y[at] == 0).all() and torch.equal(gx[at], gs[at])
+    other = torch.ones(shape, dtype=torch.bool, device="cuda")
+    other[at] = False
+    assert torch.equal(y[other], clean[0][other])
+    if checkpoint and len(shape) > 2:
+        other[0, :, :32] = False
+    assert torch.equal(gx[other], clean[1][other])
